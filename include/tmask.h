@@ -340,7 +340,132 @@ int tmask_mask_diversity(tmask_md_kind kind, int N, int M, int64_t T, double *lo
  */
 int tmask_nm_sparse_probability(int N, int M, double rho, double *prob);
 
-/* Upper bound of the workspace any call above needs for these matrices (0 on invalid arguments). */
+/*
+ * What stands around the products of a training step (the calls from here to tmask_distill_backward).
+ *
+ * A sparse model is trained, or recovered from its dense teacher, by steps whose products tmask_spmm24 computes; the
+ * calls below are what such a step does between them, forward and backward, and its loss.  They work on rows of any width:
+ * rows >= 0, cols > 0 (rows = 0: nothing is done, and column sums are 0), every leading dimension >= the row's width and
+ * < 2^31 (it does not matter for a single row), rows and cols < 2^31, pointers aligned to their element type.  Any such layout
+ * is taken; rows that begin at multiples of 16 bytes are read fastest.  `dt` is the type of activations and logits and of
+ * their gradients, `param_dt` that of weight, bias and their gradients.  All arithmetic is in fp32 and rounded once, to nearest
+ * even, where a result is stored; sums are added up in an order that depends on the sizes alone, so the same call gives the same
+ * bits.  An output may be one of the call's inputs of the same type, shape and leading dimension (in place); any other overlap
+ * is not allowed.  NaN and Inf go through the formulas.
+ */
+
+/*
+ * Layer norm, with the residual sum in front of it:
+ *     t = x + residual      mean = sum_c t / cols      rstd = 1 / sqrt(sum_c (t - mean)^2 / cols + eps)
+ *     y = (t - mean) * rstd * weight + bias                                  per row
+ * residual NULL: t = x.  weight NULL: 1, bias NULL: 0.  total, nullable and only with a residual: t is stored there, rounded to dt
+ * (y, mean and rstd are of the sum before it is rounded).  mean, rstd: fp32, one a row, both or neither (NULL).
+ * eps >= 0 and finite.
+ */
+typedef struct {
+    const void *x; int64_t ld_x;
+    const void *residual; int64_t ld_residual;
+    const void *weight, *bias;
+    void *y; int64_t ld_y;
+    void *total; int64_t ld_total;
+    float *mean, *rstd;
+    int64_t rows, cols;
+} tmask_norm_desc;
+
+int tmask_layer_norm(const tmask_norm_desc *desc, tmask_dtype dt, tmask_dtype param_dt, float eps, void *hip_stream);
+
+/*
+ * Gradients of tmask_layer_norm.  x is what was normalised (tmask_layer_norm's total, or its x without a residual), mean and
+ * rstd are its statistics; with h = (x - mean) * rstd and d = dy * weight:
+ *     dx = rstd * (d - sum_c d / cols - h * sum_c (d * h) / cols) + dtotal      (the gradient of x and of residual alike)
+ *     dweight = sum_rows dy * h      dbias = sum_rows dy
+ * dtotal, nullable: the gradient that reaches the residual stream by its other way.  weight NULL: 1.  dweight, dbias: nullable,
+ * cols elements of param_dt each.  The workspace (256-byte aligned, tmask_layer_norm_workspace_bytes(rows, cols)) is
+ * needed if one of them is asked for.
+ */
+typedef struct {
+    const void *dy; int64_t ld_dy;
+    const void *x; int64_t ld_x;
+    const float *mean, *rstd;
+    const void *weight;
+    const void *dtotal; int64_t ld_dtotal;
+    void *dx; int64_t ld_dx;
+    void *dweight, *dbias;
+    int64_t rows, cols;
+} tmask_norm_grad_desc;
+
+int tmask_layer_norm_backward(const tmask_norm_grad_desc *desc, tmask_dtype dt, tmask_dtype param_dt, void *workspace,
+                              size_t workspace_bytes, void *hip_stream);
+size_t tmask_layer_norm_workspace_bytes(int64_t rows, int64_t cols);         /* 0 on invalid sizes */
+
+/*
+ * GELU of x + bias (bias nullable: 0), with u = x + bias:
+ *     TMASK_GELU_ERF   y = u / 2 * (1 + erf(u / sqrt 2))
+ *     TMASK_GELU_TANH  y = u / 2 * (1 + tanh(sqrt(2 / pi) * (u + 0.044715 u^3)))
+ * and its gradients: dx = dy * dy/du, dbias (nullable, cols elements of param_dt) = sum_rows dx, from the same x and bias.
+ * Finite u give finite results, however large.  The workspace (256-byte aligned, tmask_bias_gelu_workspace_bytes(rows, cols)) is
+ * needed if dbias is asked for.
+ */
+typedef enum { TMASK_GELU_ERF = 0, TMASK_GELU_TANH = 1 } tmask_gelu_form;
+
+typedef struct {
+    const void *x; int64_t ld_x;
+    const void *bias;
+    void *y; int64_t ld_y;
+    int64_t rows, cols;
+} tmask_gelu_desc;
+
+typedef struct {
+    const void *dy; int64_t ld_dy;
+    const void *x; int64_t ld_x;
+    const void *bias;
+    void *dx; int64_t ld_dx;
+    void *dbias;
+    int64_t rows, cols;
+} tmask_gelu_grad_desc;
+
+int tmask_bias_gelu(const tmask_gelu_desc *desc, tmask_dtype dt, tmask_dtype param_dt, tmask_gelu_form form, void *hip_stream);
+int tmask_bias_gelu_backward(const tmask_gelu_grad_desc *desc, tmask_dtype dt, tmask_dtype param_dt, tmask_gelu_form form,
+                             void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t tmask_bias_gelu_workspace_bytes(int64_t rows, int64_t cols);          /* 0 on invalid sizes */
+
+/*
+ * Distillation from a teacher's top logits.  Row r of the student's logits z (vocab columns) is compared with a list of up to k of
+ * the teacher's: teacher[r][j], the logit, of column index[r][j].  An entry counts if its index lies in [0, vocab) and its logit is
+ * not -Inf; lists of different lengths are padded with index -1.  With temperature T:
+ *     p_j = softmax over the row's entries of teacher / T      q_v = softmax over the vocabulary of z / T
+ *     loss[r] = T^2 sum_j p_j (log p_j - log q_index(j))
+ *     dlogits[r][v] = row_weight[r] * T * (q_v - sum of p_j over the entries with index(j) = v)
+ * A row without an entry has loss 0 and gradient 0; a row whose weight is 0 (padding) has gradient 0 whatever its logits are.
+ * An index that is given several times counts several times.  A masked logit (-Inf or the type's lowest value) has q = 0: an entry
+ * for which the student has q = 0 by -Inf makes the loss +Inf, the gradient stays finite.  Logits that hold NaN or +Inf, or nothing but -Inf, make
+ * the row's loss and gradient NaN.
+ * row_max[r] = max_v z, row_sum[r] = sum_v exp((z_v - row_max) / T): nullable outputs, both or neither (q and the
+ * gradient follow from them later; row_max ignores NaN).
+ * dlogits is nullable: without it the call gives the loss alone.  row_weight (nullable: 1) is the weight of the row's loss in what is
+ * differentiated, such as 1 / tokens.  teacher is of teacher_dt, index of 32 or 64 bits (index_bits).  0 <= k <= 1024; 0 < T, finite.
+ * The workspace (256-byte aligned, tmask_distill_workspace_bytes(rows, vocab), which is 0 for sizes that need none) serves
+ * tmask_distill alone.
+ */
+typedef struct {
+    const void *logits; int64_t ld_logits;
+    const void *teacher; int64_t ld_teacher;
+    const void *index; int64_t ld_index;
+    const float *row_weight;
+    float *loss;                            /* tmask_distill alone */
+    float *row_max, *row_sum;               /* written by tmask_distill, read by tmask_distill_backward */
+    void *dlogits; int64_t ld_dlogits;
+    int64_t rows, vocab, k;
+} tmask_distill_desc;
+
+int tmask_distill(const tmask_distill_desc *desc, tmask_dtype dt, tmask_dtype teacher_dt, int index_bits, float temperature,
+                  void *workspace, size_t workspace_bytes, void *hip_stream);
+int tmask_distill_backward(const tmask_distill_desc *desc, tmask_dtype dt, tmask_dtype teacher_dt, int index_bits, float temperature,
+                           void *hip_stream);
+size_t tmask_distill_workspace_bytes(int64_t rows, int64_t vocab);           /* 0 on invalid sizes too */
+
+/* Upper bound of the workspace that any of the calls on matrices (tmask_mat and the descriptors with masks) needs for these
+ * (0 on invalid arguments). */
 size_t tmask_workspace_bytes(const tmask_mat *mats, int n_mats, int N, int M);
 
 /*

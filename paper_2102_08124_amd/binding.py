@@ -28,6 +28,8 @@ TMASK_ERR_NULL, TMASK_ERR_SHAPE, TMASK_ERR_NM, TMASK_ERR_DTYPE = -1, -2, -3, -4
 TMASK_ERR_WORKSPACE, TMASK_ERR_HIP, TMASK_ERR_ALIGN = -5, -6, -7
 
 EXPORTS = ("tmask_approx", "tmask_approx_noalloc", "tmask_exact", "tmask_prune_1d", "tmask_apply_pack", "tmask_apply_dense", "tmask_approx_dense", "tmask_prune_1d_dense", "tmask_approx_pack", "tmask_spmm24", "tmask_flip_count", "tmask_pattern_violations", "tmask_mask_diversity", "tmask_nm_sparse_probability", "tmask_score",
+           "tmask_layer_norm", "tmask_layer_norm_backward", "tmask_layer_norm_workspace_bytes", "tmask_bias_gelu", "tmask_bias_gelu_backward",
+           "tmask_bias_gelu_workspace_bytes", "tmask_distill", "tmask_distill_backward", "tmask_distill_workspace_bytes",
            "tmask_workspace_bytes", "tmask_profile_next", "tmask_last_error", "tmask_version")
 
 
@@ -77,6 +79,37 @@ class tmask_score_out(C.Structure):
     _fields_ = [("retained_l1", C.c_double), ("total_l1", C.c_double), ("kept", C.c_uint64),
                 ("row_violations", C.c_uint64), ("col_violations", C.c_uint64),
                 ("row_not_n", C.c_uint64), ("col_not_n", C.c_uint64)]
+
+
+class tmask_norm_desc(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("ld_x", C.c_int64), ("residual", C.c_void_p), ("ld_residual", C.c_int64),
+                ("weight", C.c_void_p), ("bias", C.c_void_p), ("y", C.c_void_p), ("ld_y", C.c_int64),
+                ("total", C.c_void_p), ("ld_total", C.c_int64), ("mean", C.c_void_p), ("rstd", C.c_void_p),
+                ("rows", C.c_int64), ("cols", C.c_int64)]
+
+
+class tmask_norm_grad_desc(C.Structure):
+    _fields_ = [("dy", C.c_void_p), ("ld_dy", C.c_int64), ("x", C.c_void_p), ("ld_x", C.c_int64),
+                ("mean", C.c_void_p), ("rstd", C.c_void_p), ("weight", C.c_void_p), ("dtotal", C.c_void_p), ("ld_dtotal", C.c_int64),
+                ("dx", C.c_void_p), ("ld_dx", C.c_int64), ("dweight", C.c_void_p), ("dbias", C.c_void_p),
+                ("rows", C.c_int64), ("cols", C.c_int64)]
+
+
+class tmask_gelu_desc(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("ld_x", C.c_int64), ("bias", C.c_void_p), ("y", C.c_void_p), ("ld_y", C.c_int64),
+                ("rows", C.c_int64), ("cols", C.c_int64)]
+
+
+class tmask_gelu_grad_desc(C.Structure):
+    _fields_ = [("dy", C.c_void_p), ("ld_dy", C.c_int64), ("x", C.c_void_p), ("ld_x", C.c_int64), ("bias", C.c_void_p),
+                ("dx", C.c_void_p), ("ld_dx", C.c_int64), ("dbias", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64)]
+
+
+class tmask_distill_desc(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("ld_logits", C.c_int64), ("teacher", C.c_void_p), ("ld_teacher", C.c_int64),
+                ("index", C.c_void_p), ("ld_index", C.c_int64), ("row_weight", C.c_void_p), ("loss", C.c_void_p),
+                ("row_max", C.c_void_p), ("row_sum", C.c_void_p), ("dlogits", C.c_void_p), ("ld_dlogits", C.c_int64),
+                ("rows", C.c_int64), ("vocab", C.c_int64), ("k", C.c_int64)]
 
 
 SCORE_OUT_BYTES = C.sizeof(tmask_score_out)
@@ -144,6 +177,18 @@ def load_library():
     L.tmask_nm_sparse_probability.argtypes = [ci, ci, C.c_double, C.POINTER(C.c_double)]
     L.tmask_score.restype = ci
     L.tmask_score.argtypes = [C.POINTER(tmask_mat), ci, ci, ci, ci, ci, vp, vp, vp, sz, vp]
+    for name, desc in (("tmask_layer_norm", tmask_norm_desc), ("tmask_layer_norm_backward", tmask_norm_grad_desc),
+                       ("tmask_bias_gelu", tmask_gelu_desc), ("tmask_bias_gelu_backward", tmask_gelu_grad_desc),
+                       ("tmask_distill", tmask_distill_desc), ("tmask_distill_backward", tmask_distill_desc)):
+        f = getattr(L, name)
+        f.restype = ci
+        f.argtypes = [C.POINTER(desc), ci, ci] + {"tmask_layer_norm": [C.c_float], "tmask_layer_norm_backward": [vp, sz],
+                                                  "tmask_bias_gelu": [ci], "tmask_bias_gelu_backward": [ci, vp, sz],
+                                                  "tmask_distill": [ci, C.c_float, vp, sz], "tmask_distill_backward": [ci, C.c_float]}[name] + [vp]
+    for name in ("tmask_layer_norm_workspace_bytes", "tmask_bias_gelu_workspace_bytes", "tmask_distill_workspace_bytes"):
+        f = getattr(L, name)
+        f.restype = sz
+        f.argtypes = [C.c_int64, C.c_int64]
     L.tmask_workspace_bytes.restype = sz
     L.tmask_workspace_bytes.argtypes = [C.POINTER(tmask_mat), ci, ci, ci]
     L.tmask_profile_next.restype = ci
@@ -425,6 +470,155 @@ def tmask_spmm24(vals: torch.Tensor, idx: torch.Tensor, rows: int, cols: int, x:
         raise ValueError("vals and idx must be device tensors")
     _check(L.tmask_spmm24(vals.data_ptr(), idx.data_ptr(), rows, cols, x.data_ptr(), x.stride(0),
                           y.data_ptr(), y.stride(0), x.shape[0], dtype_code(y), _stream_ptr(stream)))
+
+
+def _rows(t: Optional[torch.Tensor], what: str, shape, dtype):
+    """Address and leading dimension of a tensor of a call on rows; None stays none."""
+    if t is None:
+        return None, 0
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    p, r, c, ld = _mat2d(t, what)
+    if (r, c) != tuple(shape):
+        raise ValueError("%s must be %d x %d, got %d x %d" % ((what,) + tuple(shape) + (r, c)))
+    return p, ld
+
+
+def _vector(t: Optional[torch.Tensor], what: str, n: int, dtype):
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    if tuple(t.shape) != (n,) or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous device tensor of %d elements" % (what, n))
+    return t.data_ptr()
+
+
+def _param_dtype(*params):
+    """The common type of the weights, biases and their gradients of a call (fp32 if there are none)."""
+    dtypes = {t.dtype for t in params if t is not None}
+    if len(dtypes) > 1:
+        raise TypeError("weight, bias and their gradients share one dtype, got %s" % sorted(map(str, dtypes)))
+    return dtypes.pop() if dtypes else torch.float32
+
+
+def _dtype_code_of(dtype, what: str) -> int:
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("%s must be float32 or bfloat16, got %s" % (what, dtype))
+    return TMASK_F32 if dtype == torch.float32 else TMASK_BF16
+
+
+def _device_bytes(n: int, like: torch.Tensor) -> torch.Tensor:
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=like.device)
+
+
+def alloc_layer_norm_workspace(x: torch.Tensor) -> torch.Tensor:
+    """Workspace for tmask_layer_norm_backward of tensors of x's shape."""
+    return _device_bytes(int(load_library().tmask_layer_norm_workspace_bytes(x.shape[0], x.shape[1])), x)
+
+
+def alloc_bias_gelu_workspace(x: torch.Tensor) -> torch.Tensor:
+    """Workspace for tmask_bias_gelu_backward of tensors of x's shape."""
+    return _device_bytes(int(load_library().tmask_bias_gelu_workspace_bytes(x.shape[0], x.shape[1])), x)
+
+
+def alloc_distill_workspace(logits: torch.Tensor) -> torch.Tensor:
+    """Workspace for tmask_distill of logits of this shape."""
+    return _device_bytes(int(load_library().tmask_distill_workspace_bytes(logits.shape[0], logits.shape[1])), logits)
+
+
+def tmask_layer_norm(x: torch.Tensor, y: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                     residual: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None,
+                     rstd: Optional[torch.Tensor] = None, eps: float = 1e-5, stream=None) -> None:
+    """y = layer norm of the rows of x + residual, times weight, plus bias.  total receives x + residual; mean and rstd
+    (fp32, one a row) the statistics that tmask_layer_norm_backward needs.  x, y, residual, total share a dtype, weight and bias
+    another."""
+    L = _lib or load_library()
+    dt = _dtype_code_of(x.dtype, "x")
+    px, rows, cols, ld = _mat2d(x, "x")
+    pd = _param_dtype(weight, bias)
+    d = tmask_norm_desc(px, ld, *_rows(residual, "residual", (rows, cols), x.dtype), _vector(weight, "weight", cols, pd),
+                        _vector(bias, "bias", cols, pd), *_rows(y, "y", (rows, cols), x.dtype),
+                        *_rows(total, "total", (rows, cols), x.dtype), _vector(mean, "mean", rows, torch.float32),
+                        _vector(rstd, "rstd", rows, torch.float32), rows, cols)
+    _check(L.tmask_layer_norm(d, dt, _dtype_code_of(pd, "weight and bias"), eps, _stream_ptr(stream)))
+
+
+def tmask_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, dx: torch.Tensor,
+                              weight: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None,
+                              dbias: Optional[torch.Tensor] = None, dtotal: Optional[torch.Tensor] = None,
+                              workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of tmask_layer_norm: x is what was normalised (its total, or its x without a residual), mean and rstd its
+    statistics.  dx (plus dtotal, what reaches the residual stream by its other way) is the gradient of x and residual
+    alike; dweight and dbias need a workspace (alloc_layer_norm_workspace)."""
+    L = _lib or load_library()
+    dt = _dtype_code_of(x.dtype, "x")
+    px, rows, cols, ld = _mat2d(x, "x")
+    pd = _param_dtype(weight, dweight, dbias)
+    d = tmask_norm_grad_desc(*_rows(dy, "dy", (rows, cols), x.dtype), px, ld, _vector(mean, "mean", rows, torch.float32),
+                             _vector(rstd, "rstd", rows, torch.float32), _vector(weight, "weight", cols, pd),
+                             *_rows(dtotal, "dtotal", (rows, cols), x.dtype), *_rows(dx, "dx", (rows, cols), x.dtype),
+                             _vector(dweight, "dweight", cols, pd), _vector(dbias, "dbias", cols, pd), rows, cols)
+    wp, wb = _ws_args(workspace)
+    _check(L.tmask_layer_norm_backward(d, dt, _dtype_code_of(pd, "weight, dweight and dbias"), wp, wb, _stream_ptr(stream)))
+
+
+def tmask_bias_gelu(x: torch.Tensor, y: torch.Tensor, bias: Optional[torch.Tensor] = None, tanh: bool = False, stream=None) -> None:
+    """y = GELU(x + bias), with erf or (tanh=True) in its form with tanh."""
+    L = _lib or load_library()
+    dt = _dtype_code_of(x.dtype, "x")
+    px, rows, cols, ld = _mat2d(x, "x")
+    pd = _param_dtype(bias)
+    d = tmask_gelu_desc(px, ld, _vector(bias, "bias", cols, pd), *_rows(y, "y", (rows, cols), x.dtype), rows, cols)
+    _check(L.tmask_bias_gelu(d, dt, _dtype_code_of(pd, "bias"), 1 if tanh else 0, _stream_ptr(stream)))
+
+
+def tmask_bias_gelu_backward(dy: torch.Tensor, x: torch.Tensor, dx: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                             dbias: Optional[torch.Tensor] = None, tanh: bool = False, workspace: Optional[torch.Tensor] = None,
+                             stream=None) -> None:
+    """Gradients of tmask_bias_gelu from the same x and bias; dbias needs a workspace (alloc_bias_gelu_workspace)."""
+    L = _lib or load_library()
+    dt = _dtype_code_of(x.dtype, "x")
+    px, rows, cols, ld = _mat2d(x, "x")
+    pd = _param_dtype(bias, dbias)
+    d = tmask_gelu_grad_desc(*_rows(dy, "dy", (rows, cols), x.dtype), px, ld, _vector(bias, "bias", cols, pd),
+                             *_rows(dx, "dx", (rows, cols), x.dtype), _vector(dbias, "dbias", cols, pd), rows, cols)
+    wp, wb = _ws_args(workspace)
+    _check(L.tmask_bias_gelu_backward(d, dt, _dtype_code_of(pd, "bias and dbias"), 1 if tanh else 0, wp, wb, _stream_ptr(stream)))
+
+
+def _distill_desc(logits, teacher, index, loss, row_max, row_sum, dlogits, row_weight):
+    _dtype_code_of(logits.dtype, "logits")
+    pz, rows, vocab, ld = _mat2d(logits, "logits")
+    k = int(teacher.shape[1]) if teacher.dim() == 2 else -1
+    if index.dtype not in (torch.int32, torch.int64):
+        raise TypeError("index must be int32 or int64, got %s" % index.dtype)
+    d = tmask_distill_desc(pz, ld, *_rows(teacher, "teacher", (rows, k), teacher.dtype), *_rows(index, "index", (rows, k), index.dtype),
+                           _vector(row_weight, "row_weight", rows, torch.float32), _vector(loss, "loss", rows, torch.float32),
+                           _vector(row_max, "row_max", rows, torch.float32), _vector(row_sum, "row_sum", rows, torch.float32),
+                           *_rows(dlogits, "dlogits", (rows, vocab), logits.dtype), rows, vocab, k)
+    return d, dtype_code(logits), _dtype_code_of(teacher.dtype, "teacher"), 32 if index.dtype == torch.int32 else 64
+
+
+def tmask_distill(logits: torch.Tensor, teacher: torch.Tensor, index: torch.Tensor, temperature: float, loss: torch.Tensor,
+                  row_max: Optional[torch.Tensor] = None, row_sum: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
+                  row_weight: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """loss[r] = T^2 * KL(softmax(teacher / T) || softmax(logits / T)) of each row, the teacher's distribution being that of its top
+    logits: teacher[r][j] is the logit of column index[r][j] (int32 or int64; -1: no entry).  With dlogits the gradient of
+    sum(row_weight * loss) in the same call; row_max and row_sum are what tmask_distill_backward needs later.
+    workspace: alloc_distill_workspace."""
+    L = _lib or load_library()
+    d, dt, tdt, bits = _distill_desc(logits, teacher, index, loss, row_max, row_sum, dlogits, row_weight)
+    wp, wb = _ws_args(workspace)
+    _check(L.tmask_distill(d, dt, tdt, bits, temperature, wp, wb, _stream_ptr(stream)))
+
+
+def tmask_distill_backward(logits: torch.Tensor, teacher: torch.Tensor, index: torch.Tensor, temperature: float, row_max: torch.Tensor,
+                           row_sum: torch.Tensor, dlogits: torch.Tensor, row_weight: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dlogits = the gradient of sum(row_weight * loss) of an earlier tmask_distill, from its row_max and row_sum."""
+    L = _lib or load_library()
+    d, dt, tdt, bits = _distill_desc(logits, teacher, index, None, row_max, row_sum, dlogits, row_weight)
+    _check(L.tmask_distill_backward(d, dt, tdt, bits, temperature, _stream_ptr(stream)))
 
 
 MD_KINDS = {"unstructured": 0, "structured": 1, "transposable": 2, "sequential": 3}

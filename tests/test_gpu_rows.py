@@ -1,0 +1,565 @@
+"""Layer norm, bias + GELU and distillation on the GPU against their formulas in 64 bits; the bounds are those of row_refs.py."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2102_08124_amd import binding as tm            # noqa: E402
+from tests import row_refs as refs                        # noqa: E402
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+class Maker:
+    """Tensors on the GPU with guards: rows of `pad` elements more, the first `shift` elements into their memory, and what lies
+    between the rows is checked to be untouched."""
+
+    def __init__(self, seed, pad=0, shift=0):
+        self.gen = torch.Generator(device="cuda")
+        self.gen.manual_seed(seed)
+        self.pad, self.shift, self.buffers = pad, shift, []
+
+    def normal(self, shape, dtype, scale=1.0, mean=0.0):
+        return (torch.randn(shape, device="cuda", generator=self.gen) * scale + mean).to(dtype)
+
+    def place(self, rows, cols, dtype):
+        n = self.shift + rows * (cols + self.pad) + 64
+        buf = torch.full((n,), 7.0, dtype=dtype, device="cuda")
+        view = buf[self.shift:self.shift + rows * (cols + self.pad)].view(rows, cols + self.pad)[:, :cols]
+        self.buffers.append((buf, view))
+        return view
+
+    def put(self, t):
+        view = self.place(t.shape[0], t.shape[1], t.dtype)
+        view.copy_(t)
+        return view
+
+    def check_guards(self):
+        for buf, view in self.buffers:
+            rest = buf.clone()
+            rest[self.shift:self.shift + view.shape[0] * (view.shape[1] + self.pad)].view(view.shape[0], -1)[:, :view.shape[1]] = 7.0
+            assert bool((rest == 7.0).all()), "written outside the rows"
+
+
+def np64(t):
+    return None if t is None else t.detach().double().cpu().numpy()
+
+
+def check(got, want, what=""):
+    value, bound = want
+    g = np64(got)
+    assert g.shape == value.shape, what
+    limit = refs.stored(value, bound, got.dtype == torch.bfloat16)
+    with np.errstate(invalid="ignore"):
+        ok = (np.abs(g - value) <= limit) | (g == value) | (np.isnan(g) & np.isnan(value))
+    assert ok.all(), "%s: %d of %d outside, worst %.3g times the bound at %s" % (
+        what, (~ok).sum(), ok.size, np.nanmax(np.abs(g - value) / limit), np.argwhere(~ok)[0])
+
+
+# one lane, less and more than a wavefront, around the widths at which a row takes another kernel, longer than any registers
+WIDTHS = [1, 2, 7, 64, 65, 255, 500, 512, 513, 1000, 1023, 1024, 1025, 2048, 2050, 4096, 4097, 8192, 8200, 16384, 16391, 40000]
+
+
+def norm_call(m, rows, cols, dt, pdt, residual=True, affine=True, stats=True, mean=0.3, eps=1e-5):
+    dt, pdt = TYPES[dt], TYPES[pdt]
+    x = m.put(m.normal((rows, cols), dt, 1.0, mean))
+    res = m.put(m.normal((rows, cols), dt, 2.0)) if residual else None
+    w, b = (m.normal((cols,), pdt, 0.2, 1.0), m.normal((cols,), pdt, 0.2)) if affine else (None, None)
+    y, total = m.place(rows, cols, dt), m.place(rows, cols, dt) if residual else None
+    mu, rs = (torch.empty(rows, device="cuda") for _ in range(2)) if stats else (None, None)
+    tm.tmask_layer_norm(x, y, w, b, residual=res, total=total, mean=mu, rstd=rs, eps=eps)
+    torch.cuda.synchronize()
+    want = refs.layer_norm(np64(x), np64(res), np64(w), np64(b), float(np.float32(eps)))
+    check(y, want["y"], "y")
+    if residual:
+        check(total, want["total"], "total")
+    if stats:
+        check(mu, want["mean"], "mean")
+        check(rs, want["rstd"], "rstd")
+    m.check_guards()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_norm_widths(cols, dt):
+    for rows in (1, 3):
+        norm_call(Maker(cols), rows, cols, dt, dt)
+
+
+@pytest.mark.parametrize("dt,pdt", [("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("rows,cols", [(2, 1024), (1003, 130), (700, 1024), (300, 4100), (9000, 96)])
+def test_norm_rows_and_parameter_types(rows, cols, dt, pdt):
+    norm_call(Maker(rows), rows, cols, dt, pdt)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (5, 0), (0, 1), (3, 3), (16, 8)])
+@pytest.mark.parametrize("cols", [37, 1024, 5000])
+def test_norm_strides_and_alignment(cols, pad, shift, dt):
+    norm_call(Maker(1, pad, shift), 5, cols, dt, "f32")
+
+
+@pytest.mark.parametrize("residual,affine,stats", [(False, True, True), (True, False, True), (False, False, False)])
+@pytest.mark.parametrize("cols", [200, 1024, 20000])
+def test_norm_without_its_options(cols, residual, affine, stats):
+    norm_call(Maker(5), 4, cols, "bf16", "f32", residual, affine, stats)
+
+
+@pytest.mark.parametrize("cols", [100, 1024, 20000])
+def test_norm_far_from_zero(cols):
+    """A mean 300 times the deviation: the variance is of the differences from the mean."""
+    norm_call(Maker(9), 6, cols, "f32", "f32", residual=False, mean=300.0)
+
+
+@pytest.mark.parametrize("cols", [3, 1024, 20000])
+def test_norm_of_rows_that_hold_one_value(cols):
+    x = torch.full((3, cols), 2.5, device="cuda")
+    b = torch.arange(cols, device="cuda", dtype=torch.float32)
+    y, mu, rs = torch.empty_like(x), torch.empty(3, device="cuda"), torch.empty(3, device="cuda")
+    tm.tmask_layer_norm(x, y, None, b, mean=mu, rstd=rs, eps=1e-5)
+    torch.cuda.synchronize()
+    # a mean of equal numbers, off by 2 u of them at most, times the largest possible rstd
+    assert float((y - b).abs().max()) <= (cols / 64 + 18) * refs.U * 2.5 * 317 + cols * refs.U
+    assert bool((rs > 300).all())
+
+
+@pytest.mark.parametrize("cols", [70, 1024, 20000])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_norm_keeps_bad_rows_to_themselves(cols, bad):
+    m = Maker(2)
+    x = m.normal((7, cols), torch.bfloat16)
+    y0, y = torch.empty_like(x), torch.empty_like(x)
+    tm.tmask_layer_norm(x, y0)
+    x[3, cols // 2] = bad
+    tm.tmask_layer_norm(x, y)
+    torch.cuda.synchronize()
+    keep = [0, 1, 2, 4, 5, 6]
+    assert torch.equal(y[keep], y0[keep]) and bool(y[3].isnan().any())
+
+
+@pytest.mark.parametrize("cols", [300, 1024, 3000, 20000])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_norm_in_place(cols, dt):
+    m = Maker(4)
+    x, r = m.normal((9, cols), TYPES[dt]), m.normal((9, cols), TYPES[dt])
+    y, t = torch.empty_like(x), torch.empty_like(x)
+    tm.tmask_layer_norm(x, y, residual=r, total=t)
+    x1, r1 = x.clone(), r.clone()
+    tm.tmask_layer_norm(x1, x1, residual=r1, total=r1)
+    x2, r2 = x.clone(), r.clone()
+    tm.tmask_layer_norm(x2, r2, residual=r2, total=x2)
+    torch.cuda.synchronize()
+    assert torch.equal(x1, y) and torch.equal(r1, t) and torch.equal(r2, y) and torch.equal(x2, t)
+
+
+def grad_call(m, rows, cols, dt, pdt, more=True, affine=True, in_place=None):
+    dt, pdt = TYPES[dt], TYPES[pdt]
+    x, dy = m.put(m.normal((rows, cols), dt, 2.0, 0.3)), m.put(m.normal((rows, cols), dt, 0.3))
+    dtotal = m.put(m.normal((rows, cols), dt, 0.3)) if more else None
+    w = m.normal((cols,), pdt, 0.2, 1.0) if affine else None
+    dx = {"dy": dy, "x": x, "dtotal": dtotal}[in_place] if in_place else m.place(rows, cols, dt)
+    x64 = x.double()
+    mu, rs = x64.mean(1).float(), (x64.var(1, correction=0) + 1e-5).rsqrt().float()
+    dw, db = (torch.empty(cols, dtype=pdt, device="cuda") for _ in range(2)) if affine else (None, None)
+    want = refs.layer_norm_backward(np64(dy), np64(x), np64(mu), np64(rs), np64(w), np64(dtotal))
+    tm.tmask_layer_norm_backward(dy, x, mu, rs, dx, w, dweight=dw, dbias=db, dtotal=dtotal, workspace=tm.alloc_layer_norm_workspace(x) if affine else None)
+    torch.cuda.synchronize()
+    check(dx, want["dx"], "dx")
+    if affine:
+        check(dw, want["dweight"], "dweight")
+        check(db, want["dbias"], "dbias")
+    m.check_guards()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_norm_grad_widths(cols, dt):
+    for rows in (1, 5):
+        grad_call(Maker(cols), rows, cols, dt, dt)
+
+
+@pytest.mark.parametrize("dt,pdt", [("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("rows,cols", [(2, 1024), (1003, 130), (2500, 1024), (300, 4100), (9000, 96)])
+def test_norm_grad_rows_and_parameter_types(rows, cols, dt, pdt):
+    grad_call(Maker(rows), rows, cols, dt, pdt)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (5, 0), (0, 1), (3, 3)])
+@pytest.mark.parametrize("cols", [37, 1024, 5000])
+def test_norm_grad_strides_and_alignment(cols, pad, shift, dt):
+    grad_call(Maker(1, pad, shift), 5, cols, dt, "f32")
+
+
+@pytest.mark.parametrize("more,affine", [(False, True), (True, False), (False, False)])
+@pytest.mark.parametrize("cols", [200, 1024, 20000])
+def test_norm_grad_without_its_options(cols, more, affine):
+    grad_call(Maker(5), 4, cols, "bf16", "f32", more, affine)
+
+
+@pytest.mark.parametrize("in_place", ["dy", "x", "dtotal"])
+@pytest.mark.parametrize("cols", [300, 1024, 3000, 20000])
+def test_norm_grad_in_place(cols, in_place):
+    grad_call(Maker(6), 70, cols, "bf16", "f32", in_place=in_place)
+
+
+@pytest.mark.parametrize("which", ["dweight", "dbias"])
+def test_norm_grad_of_one_parameter(which):
+    m = Maker(8)
+    x, dy = m.normal((40, 1000), torch.float32), m.normal((40, 1000), torch.float32)
+    mu, rs = torch.zeros(40, device="cuda"), torch.ones(40, device="cuda")
+    dx, ws = torch.empty_like(x), tm.alloc_layer_norm_workspace(x)
+    both = {k: torch.empty(1000, device="cuda") for k in ("dweight", "dbias")}
+    tm.tmask_layer_norm_backward(dy, x, mu, rs, dx, workspace=ws, **both)
+    one = torch.empty(1000, device="cuda")
+    tm.tmask_layer_norm_backward(dy, x, mu, rs, dx, workspace=ws, **{which: one})
+    torch.cuda.synchronize()
+    assert torch.equal(one, both[which])
+
+
+def gelu_call(m, rows, cols, dt, pdt, tanh, affine=True, scale=2.0):
+    dt, pdt = TYPES[dt], TYPES[pdt]
+    x, dy = m.put(m.normal((rows, cols), dt, scale)), m.put(m.normal((rows, cols), dt))
+    b = m.normal((cols,), pdt, 0.3) if affine else None
+    db = torch.empty(cols, dtype=pdt, device="cuda")
+    y, dx = m.place(rows, cols, dt), m.place(rows, cols, dt)
+    tm.tmask_bias_gelu(x, y, b, tanh=tanh)
+    tm.tmask_bias_gelu_backward(dy, x, dx, b, dbias=db, tanh=tanh, workspace=tm.alloc_bias_gelu_workspace(x))
+    torch.cuda.synchronize()
+    check(y, refs.bias_gelu(np64(x), np64(b), tanh)["y"], "y")
+    want = refs.bias_gelu_backward(np64(dy), np64(x), np64(b), tanh)
+    check(dx, want["dx"], "dx")
+    check(db, want["dbias"], "dbias")
+    m.check_guards()
+
+
+@pytest.mark.parametrize("tanh", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [1, 7, 64, 255, 511, 512, 1001, 2048, 2053, 4096, 9000])
+def test_gelu_widths(cols, dt, tanh):
+    for rows in (1, 3):
+        gelu_call(Maker(cols), rows, cols, dt, dt, tanh)
+
+
+@pytest.mark.parametrize("dt,pdt", [("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("rows,cols", [(2, 1024), (1003, 130), (700, 1024), (33, 4100), (9000, 40)])
+def test_gelu_rows_and_parameter_types(rows, cols, dt, pdt):
+    gelu_call(Maker(rows), rows, cols, dt, pdt, rows % 2 == 0)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (5, 0), (0, 1), (3, 3)])
+def test_gelu_strides_and_alignment(pad, shift, dt):
+    gelu_call(Maker(1, pad, shift), 5, 1111, dt, "f32", False)
+    gelu_call(Maker(1, pad, shift), 5, 1024, dt, "f32", True, affine=False)
+
+
+@pytest.mark.parametrize("tanh", [False, True])
+def test_gelu_everywhere(tanh):
+    """Every bf16 number but the infinities and NaN, and fp32 numbers of every size."""
+    bits = torch.arange(65536, dtype=torch.int32, device="cuda").to(torch.int16)
+    x = bits.view(torch.bfloat16)
+    x = x[x.isfinite()].reshape(1, -1)
+    for t in (x, x.float() * 1.0009765625):
+        t = t[:, t.isfinite()[0]].contiguous()
+        y, dx = torch.empty_like(t), torch.empty_like(t)
+        tm.tmask_bias_gelu(t, y, tanh=tanh)
+        tm.tmask_bias_gelu_backward(torch.ones_like(t), t, dx, tanh=tanh)
+        torch.cuda.synchronize()
+        with np.errstate(over="ignore", invalid="ignore"):
+            u = np64(t)
+            near = np.clip(u, -100, 100)                        # beyond, the share is 0 or 1 in 64 bits too
+            share, slope = refs._gelu(near, None, tanh)[1:]
+        check(y, (u * share, 12 * refs.U * np.abs(u) * ((u > -100) & (share > 0) | (u > 0))), "y")
+        check(dx, (slope, 16 * refs.U * (1 + np.minimum(np.abs(u), 20.0))), "dx")
+
+
+def test_gelu_in_place():
+    m = Maker(4)
+    x, dy = m.normal((9, 777), torch.bfloat16), m.normal((9, 777), torch.bfloat16)
+    y, dx, ws = torch.empty_like(x), torch.empty_like(x), tm.alloc_bias_gelu_workspace(x)
+    db, db1, db2 = (torch.empty(777, device="cuda") for _ in range(3))
+    tm.tmask_bias_gelu(x, y)
+    tm.tmask_bias_gelu_backward(dy, x, dx, dbias=db, workspace=ws)
+    x1, x2, dy1 = x.clone(), x.clone(), dy.clone()
+    tm.tmask_bias_gelu(x1, x1)
+    tm.tmask_bias_gelu_backward(dy, x2, x2, dbias=db1, workspace=ws)
+    tm.tmask_bias_gelu_backward(dy1, x, dy1, dbias=db2, workspace=ws)
+    torch.cuda.synchronize()
+    assert torch.equal(x1, y) and torch.equal(x2, dx) and torch.equal(dy1, dx) and torch.equal(db, db1) and torch.equal(db, db2)
+
+
+def lists(m, rows, vocab, k, dtype, bits, ragged=False, repeats=False):
+    teacher = m.normal((rows, k), dtype, 3.0)
+    if repeats:
+        index = torch.randint(0, min(vocab, max(1, k // 2)), (rows, k), device="cuda", generator=m.gen)
+    else:
+        index = torch.rand((rows, vocab), device="cuda", generator=m.gen).argsort(1)[:, :k] if k else torch.zeros((rows, 0), device="cuda")
+    if ragged:
+        index = torch.where(torch.rand((rows, k), device="cuda", generator=m.gen) < 0.5, index, -1)
+        if rows > 1:
+            index[1] = -1
+    return teacher, index.to(torch.int32 if bits == 32 else torch.int64).contiguous()
+
+
+def distill_call(m, rows, vocab, k, dt="f32", tdt=None, bits=32, T=1.0, ragged=False, repeats=False, weights=True, edit=None):
+    z = m.put(m.normal((rows, vocab), TYPES[dt], 3.0))
+    teacher, index = lists(m, rows, vocab, k, TYPES[tdt or dt], bits, ragged, repeats)
+    if edit:
+        edit(z, teacher, index)
+    w = torch.rand(rows, device="cuda", generator=m.gen) - 0.3 if weights else None
+    if weights and rows > 2:
+        w[2] = 0.0
+    loss, top, total = (torch.full((rows,), 7.0, device="cuda") for _ in range(3))
+    dz, dz_later = m.place(rows, vocab, TYPES[dt]), m.place(rows, vocab, TYPES[dt])
+    ws = tm.alloc_distill_workspace(z)
+    tm.tmask_distill(z, teacher, index, T, loss, row_max=top, row_sum=total, dlogits=dz, row_weight=w, workspace=ws)
+    tm.tmask_distill_backward(z, teacher, index, T, top, total, dz_later, row_weight=w)
+    alone = torch.full((rows,), 7.0, device="cuda")
+    tm.tmask_distill(z, teacher, index, T, alone, workspace=ws)
+    torch.cuda.synchronize()
+    want = refs.distill(np64(z), np64(teacher), index.cpu().numpy(), T, np64(w))
+    for name, got in (("loss", loss), ("loss", alone), ("row_max", top), ("row_sum", total), ("dlogits", dz), ("dlogits", dz_later)):
+        check(got, want[name], name)
+    m.check_guards()
+    return z, teacher, index, loss, dz
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [1, 2, 7, 64, 130, 1000, 1024, 4097, 32000, 50021, 131072, 200003])
+def test_distill_widths(vocab, dt):
+    for rows in (1, 3):
+        distill_call(Maker(vocab), rows, vocab, min(vocab, 20), dt)
+
+
+@pytest.mark.parametrize("rows,vocab,k", [(2, 100, 1), (600, 40, 5), (1500, 700, 33), (300, 5000, 64), (40, 70000, 256)])
+@pytest.mark.parametrize("dt,tdt,bits,T", [("f32", "bf16", 64, 2.0), ("bf16", "f32", 32, 0.5), ("bf16", "bf16", 64, 1.0)])
+def test_distill_rows_lists_and_types(rows, vocab, k, dt, tdt, bits, T):
+    distill_call(Maker(rows), rows, vocab, k, dt, tdt, bits, T, ragged=True)
+
+
+@pytest.mark.parametrize("k", [0, 1, 63, 64, 65, 256, 257, 1000, 1024])
+def test_distill_list_lengths(k):
+    distill_call(Maker(k), 4, 2000, k, "f32", T=1.5)
+    distill_call(Maker(k), 4, 2000, k, "bf16", T=1.5, ragged=k > 0)
+
+
+@pytest.mark.parametrize("k", [2, 50, 300, 1024])
+@pytest.mark.parametrize("vocab", [3, 1500, 90000])
+def test_distill_indexes_that_repeat(vocab, k):
+    distill_call(Maker(k), 3, vocab, k, "f32", repeats=True, ragged=True)
+
+
+@pytest.mark.parametrize("pad,shift", [(8, 0), (5, 0), (0, 1), (3, 3)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_distill_strides_and_alignment(pad, shift, dt):
+    for vocab in (90, 5000, 70001):
+        distill_call(Maker(1, pad, shift), 5, vocab, 16, dt)
+
+
+def test_distill_without_weights():
+    distill_call(Maker(3), 5, 1234, 16, "bf16", weights=False)
+
+
+@pytest.mark.parametrize("vocab", [50, 3000, 100000])
+@pytest.mark.parametrize("low", [-float("inf"), torch.finfo(torch.float32).min, torch.finfo(torch.bfloat16).min])
+def test_distill_masked_logits(vocab, low):
+    """Two thirds of the vocabulary masked, with -Inf or the types' lowest values; entries only where nothing is masked, but for
+    one whose teacher's logit is masked too."""
+    def edit(z, teacher, index):
+        z[:, vocab // 3:] = low
+        index.copy_(torch.arange(index.shape[1], device="cuda").expand_as(index))
+        teacher[:, 3] = -float("inf")
+        index[:, 3] = vocab - 1
+    for dt in ("f32", "bf16"):
+        for T in (0.25, 1.0):
+            distill_call(Maker(7), 4, vocab, 8, dt, T=T, edit=edit)
+
+
+@pytest.mark.parametrize("vocab", [50, 3000, 100000])
+def test_distill_all_logits_at_the_lowest_value(vocab):
+    """A row that holds one value, however low, is the uniform distribution."""
+    def edit(z, teacher, index):
+        z[1] = torch.finfo(z.dtype).min
+    distill_call(Maker(7), 4, vocab, 8, "f32", T=0.5, edit=edit)
+
+
+@pytest.mark.parametrize("vocab", [50, 3000, 100000])
+def test_distill_entry_on_a_masked_column(vocab):
+    def edit(z, teacher, index):
+        index[0, 0] = 5
+        index[0, 1:] = -1
+        z[0, 5] = -float("inf")
+    _, _, _, loss, dz = distill_call(Maker(7), 4, vocab, 8, "f32", edit=edit)
+    assert float(loss[0]) == float("inf") and bool(dz.isfinite().all())
+
+
+@pytest.mark.parametrize("vocab", [50, 3000, 100000])
+def test_distill_teachers_lists_without_an_entry(vocab):
+    def edit(z, teacher, index):
+        teacher[0] = -float("inf")
+        index[1] = vocab                                        # outside: no entry either
+        index[3] = -2 ** 31
+        z[0, 2] = float("nan")                                  # the row has gradient 0 all the same
+        z[2] = -float("inf")                                    # its weight is 0
+    z, _, _, loss, dz = distill_call(Maker(7), 5, vocab, 8, "f32", edit=edit)
+    assert not dz[:4].any() and not loss[[0, 1, 3]].any()
+
+
+@pytest.mark.parametrize("vocab", [50, 3000, 100000])
+@pytest.mark.parametrize("bad", ["nan", "inf", "all -inf"])
+def test_distill_keeps_bad_rows_to_themselves(vocab, bad):
+    m = Maker(11)
+    z = m.normal((5, vocab), torch.float32, 3.0)
+    teacher, index = lists(m, 5, vocab, 8, torch.float32, 32)
+    out = []
+    for spoil in (False, True):
+        if spoil:
+            z[3] = z[3] if bad != "all -inf" else -float("inf")
+            z[3, vocab // 2] = {"nan": float("nan"), "inf": float("inf"), "all -inf": -float("inf")}[bad]
+        loss, dz = torch.empty(5, device="cuda"), torch.empty_like(z)
+        tm.tmask_distill(z, teacher, index, 1.0, loss, dlogits=dz, workspace=tm.alloc_distill_workspace(z))
+        out.append((loss, dz))
+    torch.cuda.synchronize()
+    keep = [0, 1, 2, 4]
+    assert torch.equal(out[0][0][keep], out[1][0][keep]) and torch.equal(out[0][1][keep], out[1][1][keep])
+    assert bool(out[1][0][3].isnan()) and bool(out[1][1][3].isnan().all())
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(3, 100), (300, 3000), (3, 100000)])
+def test_distill_in_place(rows, vocab, dt):
+    m = Maker(4)
+    z = m.normal((rows, vocab), TYPES[dt], 3.0)
+    teacher, index = lists(m, rows, vocab, 16, TYPES[dt], 32)
+    loss, loss1, top, total = (torch.empty(rows, device="cuda") for _ in range(4))
+    dz, z1, z2, ws = torch.empty_like(z), z.clone(), z.clone(), tm.alloc_distill_workspace(z)
+    tm.tmask_distill(z, teacher, index, 1.0, loss, row_max=top, row_sum=total, dlogits=dz, workspace=ws)
+    tm.tmask_distill(z1, teacher, index, 1.0, loss1, dlogits=z1, workspace=ws)
+    tm.tmask_distill_backward(z2, teacher, index, 1.0, top, total, z2)
+    torch.cuda.synchronize()
+    assert torch.equal(loss, loss1) and torch.equal(z1, dz) and torch.equal(z2, dz)
+
+
+def far(m, rows, cols, dtype):
+    """Rows 2^30 + 8 elements apart: the third begins past 2^31 elements (2^32 bytes in bf16, 2^33 in fp32)."""
+    pitch = 2 ** 30 + 8
+    buf = torch.empty(pitch * (rows - 1) + cols, dtype=dtype, device="cuda")
+    view = buf.as_strided((rows, cols), (pitch, 1))
+    view.copy_(m.normal((rows, cols), dtype, 2.0))
+    return view
+
+
+def test_rows_past_32_bits():
+    m, bf = Maker(12), torch.bfloat16
+    x, y = far(m, 4, 1000, bf), far(m, 4, 1000, bf)
+    near, out = x.contiguous(), torch.empty((4, 1000), dtype=bf, device="cuda")
+    mu, rs, a, b = (torch.empty(4, device="cuda") for _ in range(4))
+    ws, sums = tm.alloc_layer_norm_workspace(near), [torch.empty(1000, dtype=bf, device="cuda") for _ in range(4)]
+
+    def same():
+        torch.cuda.synchronize()
+        assert torch.equal(y.contiguous(), out)
+
+    tm.tmask_layer_norm(x, y, mean=mu, rstd=rs)
+    tm.tmask_layer_norm(near, out)
+    same()
+    tm.tmask_layer_norm_backward(x, x, mu, rs, y, dweight=sums[0], dbias=sums[1], workspace=ws)
+    tm.tmask_layer_norm_backward(near, near, mu, rs, out, dweight=sums[2], dbias=sums[3], workspace=ws)
+    same()
+    assert torch.equal(sums[0], sums[2]) and torch.equal(sums[1], sums[3])
+    tm.tmask_bias_gelu(x, y)
+    tm.tmask_bias_gelu(near, out)
+    same()
+    tm.tmask_bias_gelu_backward(x, x, y, dbias=sums[0], workspace=ws)
+    tm.tmask_bias_gelu_backward(near, near, out, dbias=sums[1], workspace=ws)
+    same()
+    assert torch.equal(sums[0], sums[1])
+    teacher, index = lists(m, 4, 1000, 9, bf, 32)
+    wsd = tm.alloc_distill_workspace(near)
+    tm.tmask_distill(x, teacher, index, 1.0, a, row_max=mu, row_sum=rs, dlogits=y, workspace=wsd)
+    tm.tmask_distill(near, teacher, index, 1.0, b, dlogits=out, workspace=wsd)
+    same()
+    assert torch.equal(a, b)
+    tm.tmask_distill_backward(x, teacher, index, 1.0, mu, rs, y)
+    same()
+
+
+def test_no_rows():
+    x = torch.empty((0, 64), dtype=torch.bfloat16, device="cuda")
+    none = torch.empty(0, device="cuda")
+    dw, db = torch.full((64,), 7.0, device="cuda"), torch.full((64,), 7.0, device="cuda")
+    ws = tm.alloc_layer_norm_workspace(x)
+    tm.tmask_layer_norm(x, x, mean=none, rstd=none)
+    tm.tmask_layer_norm_backward(x, x, none, none, x, dweight=dw, dbias=db, workspace=ws)
+    tm.tmask_bias_gelu(x, x)
+    index = torch.empty((0, 4), dtype=torch.int32, device="cuda")
+    tm.tmask_distill(x, x[:, :4], index, 1.0, none, dlogits=x)
+    tm.tmask_distill_backward(x, x[:, :4], index, 1.0, none, none, x)
+    torch.cuda.synchronize()
+    assert not dw.any() and not db.any()
+    db.fill_(7.0)
+    tm.tmask_bias_gelu_backward(x, x, x, dbias=db, workspace=ws)
+    torch.cuda.synchronize()
+    assert not db.any()
+
+
+def every_call(m, rows=70, cols=1500):
+    """(call, outputs) of each operator"""
+    x, dy = m.normal((rows, cols), torch.bfloat16), m.normal((rows, cols), torch.bfloat16)
+    teacher, index = lists(m, rows, cols, 12, torch.bfloat16, 32)
+    o = lambda *s: torch.empty(s or (rows, cols), dtype=torch.float32 if s else torch.bfloat16, device="cuda")   # noqa: E731
+    y, t, mu, rs, dx, dw, db, g, dg, dbg = o(), o(), o(rows), o(rows), o(), o(cols), o(cols), o(), o(), o(cols)
+    loss, top, total, dz, dz2 = o(rows), o(rows), o(rows), o(), o()
+    wsn, wsg, wsd = tm.alloc_layer_norm_workspace(x), tm.alloc_bias_gelu_workspace(x), tm.alloc_distill_workspace(x)
+
+    def call(stream=None):
+        tm.tmask_layer_norm(x, y, residual=dy, total=t, mean=mu, rstd=rs, stream=stream)
+        tm.tmask_layer_norm_backward(dy, t, mu, rs, dx, dweight=dw, dbias=db, workspace=wsn, stream=stream)
+        tm.tmask_bias_gelu(x, g, stream=stream)
+        tm.tmask_bias_gelu_backward(dy, x, dg, dbias=dbg, workspace=wsg, stream=stream)
+        tm.tmask_distill(x, teacher, index, 2.0, loss, row_max=top, row_sum=total, dlogits=dz, workspace=wsd, stream=stream)
+        tm.tmask_distill_backward(x, teacher, index, 2.0, top, total, dz2, stream=stream)
+
+    return call, [y, t, mu, rs, dx, dw, db, g, dg, dbg, loss, top, total, dz, dz2], [x, dy]
+
+
+@pytest.mark.parametrize("rows,cols", [(70, 1500), (3, 70000)])
+def test_the_same_call_gives_the_same_bits_on_any_stream(rows, cols):
+    call, outs, _ = every_call(Maker(13), rows, cols)
+    call()
+    torch.cuda.synchronize()
+    first = [t.clone() for t in outs]
+    side = torch.cuda.Stream()
+    for stream in (None, side):
+        for t in outs:
+            t.fill_(7.0)
+        torch.cuda.synchronize()
+        call(stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, outs))
+
+
+@pytest.mark.parametrize("rows,cols", [(70, 1500), (3, 70000)])
+def test_calls_in_a_graph(rows, cols):
+    """Replays, with new inputs and eager work in between, give what the calls give."""
+    call, outs, ins = every_call(Maker(14), rows, cols)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    for k in range(4):
+        for t in ins:
+            t.copy_(torch.randn(t.shape, device="cuda"))
+        for t in outs:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, outs)), k
