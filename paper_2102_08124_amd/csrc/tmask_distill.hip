@@ -11,130 +11,489 @@
 
 namespace tmask {
 
-constexpr int kMaxEntries = 1024;         // of a row's list
+constexpr uint32_t kMaxEntries = 1024;    // of a row's list
+constexpr uint32_t kMaxParts = 64;        // of a row: a lane of a wavefront has one each
+constexpr uint32_t kSlice = 256;          // threads of the kernels that work on a part of a row
 
 struct DistillArgs {
     const void *logits, *teacher, *index;
     const float *row_weight;
     float *loss, *row_max, *row_sum;
     void *dlogits;
+    float *part_stats;                    // rows x parts x {maximum, sum}
+    float *list_logits;                   // rows x k: the student's logits of the entries
     size_t ld_logits, ld_teacher, ld_index, ld_dlogits;
     uint32_t rows, vocab, k;
-    float temperature;
+    uint32_t full, tail;                  // chunks of a row, and the elements behind them (fewer than a chunk's)
+    uint32_t parts, part_chunks;
+    uint32_t teacher_f32, index64;
+    uint32_t hash_shift;
+    float temperature, per_t, per_t2;     // T, 1 / T, log2(e) / T
 };
 
-// A row's list in LDS: columns (-1: no entry), teacher's probabilities, student's logits.
+// A row's list in LDS, k numbers each: columns (-1: no entry), the teacher's logits (later: its probabilities), the student's logits.
+// table: the columns hashed, to see whether one is there twice.
 struct List {
-    int32_t at[kMaxEntries];
-    float p[kMaxEntries];
-    float z[kMaxEntries];
+    int32_t *at;
+    float *t, *z;
+    int32_t *table, *repeats;
 };
 
-// Fills `list`; the result, the same in every thread: whether the row has an entry.  log_p_shift: log p_j = (t_j - its maximum) / T
-// - log_p_shift.  p holds (t_j - maximum) / T until the caller has used it: see list_softmax.
-template <int DT, int TDT, int IDX>
-__device__ __forceinline__ bool read_list(const DistillArgs &a, uint32_t r, List &list, float *red, float &log_sum, float &t_max)
+__device__ __forceinline__ List list_in(void *lds, const DistillArgs &a)
 {
-    float m = -INFINITY, some = 0.f;
-    for (uint32_t j = threadIdx.x; j < a.k; j += kThreads) {
-        const int64_t at = IDX == 32 ? (int64_t)((const int32_t *)a.index)[r * a.ld_index + j] : ((const int64_t *)a.index)[r * a.ld_index + j];
-        const float t = load_one<TDT>(a.teacher, r * a.ld_teacher + j);
-        const bool counts = at >= 0 && at < (int64_t)a.vocab && t != -INFINITY;
-        list.at[j] = counts ? (int32_t)at : -1;
-        list.p[j] = t;
-        list.z[j] = counts ? load_one<DT>(a.logits, r * a.ld_logits + (size_t)at) : 0.f;
-        if (counts) {
-            m = fmaxf(m, t);
-            some = 1.f;
-        }
-    }
-    t_max = group_max<kThreads / 64>(m, red);
-    some = group_max<kThreads / 64>(some, red);
-    float s = 0.f;
-    for (uint32_t j = threadIdx.x; j < a.k; j += kThreads)
-        if (list.at[j] >= 0)
-            s += expf((list.p[j] - t_max) / a.temperature);
-    log_sum = logf(group_sum<kThreads / 64>(s, red));
-    return some > 0.f;
+    List l;
+    l.repeats = (int32_t *)lds;
+    l.at = l.repeats + 4;
+    l.t = (float *)l.at + a.k;
+    l.z = l.t + a.k;
+    l.table = (int32_t *)l.z + a.k;
+    return l;
 }
 
-// what the entries take from column `at`: the sum of their probabilities
-__device__ __forceinline__ float share_of(const List &list, uint32_t k, int32_t at)
+static size_t list_bytes(uint32_t k, uint32_t hash_shift) { return 4u * (4u + 3u * k + (k ? 1u << (32u - hash_shift) : 0u)); }
+
+// exp(x / T) for x <= 0
+__device__ __forceinline__ float exp_of(const DistillArgs &a, float x) { return __builtin_amdgcn_exp2f(x * a.per_t2); }
+
+// Entry j of row r, written to the list; the result is its logit if it counts, +Inf for NaN, else -Inf.
+__device__ __forceinline__ float read_entry(const DistillArgs &a, uint32_t r, uint32_t j, const List &l)
+{
+    const size_t i = r * a.ld_index + j, k = r * a.ld_teacher + j;
+    const int64_t at = a.index64 ? ((const int64_t *)a.index)[i] : (int64_t)((const int32_t *)a.index)[i];
+    const float t = a.teacher_f32 ? load_one<kF32>(a.teacher, k) : load_one<kBF16>(a.teacher, k);
+    const bool counts = at >= 0 && at < (int64_t)a.vocab && t != -INFINITY;
+    l.at[j] = counts ? (int32_t)at : -1;
+    l.t[j] = t;
+    return !counts ? -INFINITY : t != t ? INFINITY : t;
+}
+
+// Notes whether `at` has been entered before.  The table has at least twice as many places as the list has entries, so the search
+// ends.
+__device__ __forceinline__ void enter(const DistillArgs &a, const List &l, int32_t at)
+{
+    const uint32_t mask = (1u << (32u - a.hash_shift)) - 1u;
+    uint32_t h = ((uint32_t)at * 2654435769u) >> a.hash_shift;
+    for (;;) {
+        const int32_t was = atomicCAS(&l.table[h], -1, at);
+        if (was == -1)
+            return;
+        if (was == at) {
+            *l.repeats = 1;
+            return;
+        }
+        h = (h + 1u) & mask;
+    }
+}
+
+template <uint32_t T>
+__device__ __forceinline__ void clear_table(const DistillArgs &a, const List &l)
+{
+    for (uint32_t i = threadIdx.x; i < 1u << (32u - a.hash_shift); i += T)
+        l.table[i] = -1;
+    if (threadIdx.x == 0)
+        *l.repeats = 0;
+}
+
+// what the entries take from column `at`: the sum of their probabilities, in the list's order
+__device__ __forceinline__ float share_of(const DistillArgs &a, const List &l, int32_t at)
 {
     float s = 0.f;
-    for (uint32_t j = 0; j < k; j++)
-        if (list.at[j] == at)
-            s += list.p[j];
+    for (uint32_t j = 0; j < a.k; j++)
+        s += l.at[j] == at ? l.t[j] : 0.f;
     return s;
 }
 
-template <int DT>
-__device__ __forceinline__ void write_gradient(const DistillArgs &a, uint32_t r, List &list, bool some, float z_max, float z_sum, float t_max, float t_log_sum)
+// ---------------------------------------------------------------------------------------------------------------------
+// A row in the registers of one workgroup: T threads with P chunks each.  The logits are read once; the maximum, the sum and
+// the gradient are taken from registers.  (The chunk that a row ends inside, if its length is odd, is thread 0's.)
+//
+// The gradient's columns that the list names are written again, with what the teacher takes from them, when the rest has been
+// written: k of the vocabulary's columns, and the barrier between orders the two.
+// ---------------------------------------------------------------------------------------------------------------------
+template <int DT, int T, int P>
+__global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
 {
-    const float w = (a.row_weight ? a.row_weight[r] : 1.f) * a.temperature;
-    const size_t z0 = r * a.ld_logits, d0 = r * a.ld_dlogits;
-    const bool none = !some || w == 0.f;
-    for (uint32_t j = threadIdx.x; j < a.k; j += kThreads)
-        if (list.at[j] >= 0)
-            list.p[j] = expf((list.p[j] - t_max) / a.temperature - t_log_sum);
-    __syncthreads();
-    for (uint32_t v = threadIdx.x; v < a.vocab; v += kThreads)
-        store_one<DT>(a.dlogits, d0 + v, none ? 0.f : w * (expf((load_one<DT>(a.logits, z0 + v) - z_max) / a.temperature) / z_sum));
-    __syncthreads();
-    for (uint32_t j = threadIdx.x; j < a.k && !none; j += kThreads)
-        if (list.at[j] >= 0)
-            store_one<DT>(a.dlogits, d0 + (uint32_t)list.at[j],
-                          w * (expf((list.z[j] - z_max) / a.temperature) / z_sum - share_of(list, a.k, list.at[j])));
-    __syncthreads();
-}
-
-template <int DT, int TDT, int IDX>
-__global__ void __launch_bounds__(kThreads) distill_kernel(const DistillArgs a)
-{
-    __shared__ float red[kThreads / 64];
-    __shared__ List list;
+    constexpr int N = kElems<DT>, W = T / 64;
+    constexpr uint32_t kNone = DT == kF32 ? 0xFF800000u : 0xFF80FF80u;          // -Inf
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    float *const red = (float *)lds;                                            // 2 x 2 W numbers, and W
+    const List list = list_in(red + 5 * W, a);
     for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        float t_log_sum, t_max;
-        const bool some = read_list<DT, TDT, IDX>(a, r, list, red, t_log_sum, t_max);
         const size_t z0 = r * a.ld_logits;
-        float m = -INFINITY;
-        for (uint32_t v = threadIdx.x; v < a.vocab; v += kThreads)
-            m = fmaxf(m, load_one<DT>(a.logits, z0 + v));
-        const float z_max = group_max<kThreads / 64>(m, red);
-        float s = 0.f;
-        for (uint32_t v = threadIdx.x; v < a.vocab; v += kThreads)
-            s += expf((load_one<DT>(a.logits, z0 + v) - z_max) / a.temperature);
-        const float z_sum = group_sum<kThreads / 64>(s, red), z_log_sum = logf(z_sum);
-        float loss = 0.f;
-        for (uint32_t j = threadIdx.x; j < a.k; j += kThreads)
-            if (list.at[j] >= 0) {
-                const float log_p = (list.p[j] - t_max) / a.temperature - t_log_sum, log_q = (list.z[j] - z_max) / a.temperature - z_log_sum;
-                loss += log_q == -INFINITY ? INFINITY : expf(log_p) * (log_p - log_q);
+        u32x4 raw[P], last = u32x4{kNone, kNone, kNone, kNone};
+        const bool has_last = a.tail && threadIdx.x == 0;
+#pragma unroll
+        for (int i = 0; i < P; i++) {
+            const uint32_t c = threadIdx.x + (uint32_t)(i * T);
+            raw[i] = u32x4{kNone, kNone, kNone, kNone};
+            if (c < a.full)
+                raw[i] = load_chunk<DT>(a.logits, z0 + (size_t)c * N, N);
+        }
+        if (has_last)
+            last = load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail, -INFINITY);
+        float t_max = -INFINITY, z_max = -INFINITY;
+        if (a.k) {
+            clear_table<T>(a, list);
+            __syncthreads();
+            for (uint32_t j = threadIdx.x; j < a.k; j += T) {
+                t_max = fmaxf(t_max, read_entry(a, r, j, list));
+                const int32_t at = list.at[j];
+                if (at >= 0) {
+                    list.z[j] = load_one<DT>(a.logits, z0 + (uint32_t)at);
+                    if (a.dlogits)
+                        enter(a, list, at);
+                }
             }
-        loss = group_sum<kThreads / 64>(loss, red);
+        }
+        float v[N];
+#pragma unroll
+        for (int i = 0; i < P; i++) {
+            unpack<DT>(raw[i], v);
+#pragma unroll
+            for (int e = 0; e < N; e++)
+                z_max = fmaxf(z_max, v[e]);
+        }
+        unpack<DT>(last, v);
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            z_max = fmaxf(z_max, v[e]);
+        group_reduce<Max, Max, W>(t_max, z_max, red);
+
+        float t_sum = 0.f, z_sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < P; i++)
+            if ((uint32_t)(i * T) < a.full) {
+                unpack<DT>(raw[i], v);
+#pragma unroll
+                for (int e = 0; e < N; e++)
+                    z_sum += exp_of(a, v[e] - z_max);
+            }
+        if (has_last) {
+            unpack<DT>(last, v);
+#pragma unroll
+            for (int e = 0; e < N; e++)
+                z_sum += exp_of(a, v[e] - z_max);
+        }
+        for (uint32_t j = threadIdx.x; j < a.k; j += T)
+            if (list.at[j] >= 0)
+                t_sum += exp_of(a, list.t[j] - t_max);
+        group_reduce<Sum, Sum, W>(t_sum, z_sum, red + 2 * W);
+
+        const bool some = t_max != -INFINITY;
+        const float t_log = logf(t_sum), z_log = logf(z_sum), t_part = 1.f / t_sum;
+        float loss = 0.f;
+        for (uint32_t j = threadIdx.x; j < a.k; j += T)
+            if (list.at[j] >= 0) {
+                const float t = list.t[j] - t_max, p = exp_of(a, t) * t_part;
+                const float log_q = (list.z[j] - z_max) * a.per_t - z_log;
+                loss += log_q == -INFINITY ? INFINITY : p * ((t * a.per_t - t_log) - log_q);
+                list.t[j] = p;
+            }
+        loss = lanes_reduce<Sum, 64>(loss);
+        if ((threadIdx.x & 63) == 0)
+            red[4 * W + (threadIdx.x >> 6)] = loss;
+
+        const float g = a.dlogits ? (a.row_weight ? a.row_weight[r] : 1.f) * a.temperature : 0.f;
+        const float g_q = g / z_sum;
+        const bool none = !some || g == 0.f;
+        const size_t d0 = r * a.ld_dlogits;
+        if (a.dlogits) {
+#pragma unroll
+            for (int i = 0; i < P; i++) {
+                const uint32_t c = threadIdx.x + (uint32_t)(i * T);
+                if (c < a.full) {
+                    unpack<DT>(raw[i], v);
+#pragma unroll
+                    for (int e = 0; e < N; e++)
+                        v[e] = none ? 0.f : exp_of(a, v[e] - z_max) * g_q;
+                    store_chunk<DT>(a.dlogits, d0 + (size_t)c * N, N, pack<DT>(v));
+                }
+            }
+            if (has_last) {
+                unpack<DT>(last, v);
+#pragma unroll
+                for (int e = 0; e < N; e++)
+                    v[e] = none ? 0.f : exp_of(a, v[e] - z_max) * g_q;
+                store_chunk<DT>(a.dlogits, d0 + (size_t)a.full * N, a.tail, pack<DT>(v));
+            }
+        }
+        __syncthreads();
         if (threadIdx.x == 0) {
-            a.loss[r] = some ? a.temperature * a.temperature * loss : 0.f;
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; w++)
+                sum += red[4 * W + w];
+            a.loss[r] = some ? a.temperature * a.temperature * sum : 0.f;
             if (a.row_max) {
                 a.row_max[r] = z_max;
                 a.row_sum[r] = z_sum;
             }
         }
-        if (a.dlogits)
-            write_gradient<DT>(a, r, list, some, z_max, z_sum, t_max, t_log_sum);
+        if (a.dlogits && !none) {
+            const bool repeats = *list.repeats != 0;
+            for (uint32_t j = threadIdx.x; j < a.k; j += T) {
+                const int32_t at = list.at[j];
+                if (at >= 0)
+                    store_one<DT>(a.dlogits, d0 + (uint32_t)at, exp_of(a, list.z[j] - z_max) * g_q - g * (repeats ? share_of(a, list, at) : list.t[j]));
+            }
+        }
+        if (r + gridDim.x < a.rows)
+            __syncthreads();                                                    // the list and `red` are used again
     }
 }
 
-template <int DT, int TDT, int IDX>
-__global__ void __launch_bounds__(kThreads) distill_grad_kernel(const DistillArgs a)
+// ---------------------------------------------------------------------------------------------------------------------
+// Few rows, or rows that no workgroup holds: parts of rows.  The first launch takes the maximum and the sum of each part
+// (relative to its own maximum, or to 0 where that is -Inf, so that a part that is masked has sum 0) and the student's logits of the
+// entries in it; the second joins them and does the rest, part by part, from logits that the caches may still hold.
+// ---------------------------------------------------------------------------------------------------------------------
+struct Part {
+    uint32_t r, part, begin, end;         // row, part, chunks
+    bool last;                            // the row's last part: the elements behind the chunks are its own
+};
+
+__device__ __forceinline__ Part part_of(const DistillArgs &a, uint64_t id)
 {
-    __shared__ float red[kThreads / 64];
-    __shared__ List list;
-    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        float t_log_sum, t_max;
-        const bool some = read_list<DT, TDT, IDX>(a, r, list, red, t_log_sum, t_max);
-        write_gradient<DT>(a, r, list, some, a.row_max[r], a.row_sum[r], t_max, t_log_sum);
+    Part p;
+    p.r = (uint32_t)(id / a.parts);
+    p.part = (uint32_t)(id % a.parts);
+    p.begin = p.part * a.part_chunks;
+    p.last = p.part + 1u == a.parts;
+    p.end = p.last ? a.full : p.begin + a.part_chunks;
+    return p;
+}
+
+template <int DT>
+__device__ __forceinline__ bool in_part(const DistillArgs &a, const Part &p, int32_t at)
+{
+    constexpr uint32_t N = kElems<DT>;
+    return at >= 0 && (uint32_t)at >= p.begin * N && (p.last || (uint32_t)at < p.end * N);
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kSlice) distill_part_kernel(const DistillArgs a)
+{
+    constexpr int N = kElems<DT>, W = kSlice / 64, P = 4;
+    constexpr uint32_t kNone = DT == kF32 ? 0xFF800000u : 0xFF80FF80u;
+    __shared__ float red[4 * W];
+    for (uint64_t id = blockIdx.x; id < (uint64_t)a.rows * a.parts; id += gridDim.x) {
+        const Part p = part_of(a, id);
+        const size_t z0 = p.r * a.ld_logits;
+        float z_max = -INFINITY, z_sum = 0.f, v[N];
+        for (uint32_t c0 = p.begin; c0 < p.end || (c0 == p.begin && p.last); c0 += P * kSlice) {
+            u32x4 raw[P + 1];
+            float m = z_max;
+#pragma unroll
+            for (int i = 0; i <= P; i++)
+                raw[i] = u32x4{kNone, kNone, kNone, kNone};
+#pragma unroll
+            for (int i = 0; i < P; i++) {
+                const uint32_t c = c0 + threadIdx.x + (uint32_t)i * kSlice;
+                if (c < p.end)
+                    raw[i] = load_chunk<DT>(a.logits, z0 + (size_t)c * N, N);
+            }
+            const bool tail = a.tail && p.last && c0 == p.begin && threadIdx.x == 0;
+            if (tail)
+                raw[P] = load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail, -INFINITY);
+#pragma unroll
+            for (int i = 0; i <= P; i++) {
+                unpack<DT>(raw[i], v);
+#pragma unroll
+                for (int e = 0; e < N; e++)
+                    m = fmaxf(m, v[e]);
+            }
+            const float to = m == -INFINITY ? 0.f : m;
+            z_sum *= z_max == -INFINITY ? 1.f : exp_of(a, z_max - to);           // from 0 to a maximum: the sum is 0 or NaN
+            z_max = m;
+#pragma unroll
+            for (int i = 0; i <= P; i++)
+                if (i < P || tail) {
+                    unpack<DT>(raw[i], v);
+#pragma unroll
+                    for (int e = 0; e < N; e++)
+                        z_sum += exp_of(a, v[e] - to);
+                }
+        }
+        float all = z_max, unused = 0.f;
+        group_reduce<Max, Max, W>(all, unused, red);
+        z_sum *= z_max == -INFINITY ? 1.f : exp_of(a, z_max - all);
+        group_reduce<Sum, Sum, W>(z_sum, unused, red + 2 * W);
+        if (threadIdx.x == 0) {
+            a.part_stats[2 * id] = all;
+            a.part_stats[2 * id + 1] = z_sum;
+        }
+        for (uint32_t j = threadIdx.x; j < a.k; j += kSlice) {
+            const size_t i = p.r * a.ld_index + j;
+            const int64_t at = a.index64 ? ((const int64_t *)a.index)[i] : (int64_t)((const int32_t *)a.index)[i];
+            if (at < (int64_t)a.vocab && in_part<DT>(a, p, at < 0 ? -1 : (int32_t)at))
+                a.list_logits[(size_t)p.r * a.k + j] = load_one<DT>(a.logits, z0 + (size_t)at);
+        }
+        if (id + gridDim.x < (uint64_t)a.rows * a.parts)
+            __syncthreads();
     }
 }
+
+// JOIN: after distill_part_kernel, with the loss; otherwise the gradient from the row's statistics.
+template <int DT, bool JOIN>
+__global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs a)
+{
+    constexpr int N = kElems<DT>, W = kSlice / 64, P = 4;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    float *const red = (float *)lds;
+    const List list = list_in(red + 5 * W, a);
+    for (uint64_t id = blockIdx.x; id < (uint64_t)a.rows * a.parts; id += gridDim.x) {
+        const Part p = part_of(a, id);
+        if (JOIN && !a.dlogits && p.part)                                       // the loss alone is joined by one workgroup a row
+            continue;
+        const size_t z0 = p.r * a.ld_logits;
+        float z_max, z_sum;
+        if constexpr (JOIN) {
+            const uint32_t lane = threadIdx.x & 63;
+            float m = -INFINITY, s = 0.f;
+            if (lane < a.parts) {
+                m = a.part_stats[2 * ((uint64_t)p.r * a.parts + lane)];
+                s = a.part_stats[2 * ((uint64_t)p.r * a.parts + lane) + 1];
+            }
+            z_max = lanes_reduce<Max, 64>(m);
+            // all parts masked: NaN, as for a row in registers
+            z_sum = lanes_reduce<Sum, 64>(lane >= a.parts ? 0.f : m == -INFINITY && z_max != -INFINITY ? s : s * exp_of(a, m - z_max));
+        } else {
+            z_max = a.row_max[p.r];
+            z_sum = a.row_sum[p.r];
+        }
+        float t_max = -INFINITY, t_sum = 0.f, unused = 0.f;
+        if (a.k) {
+            if (a.dlogits) {
+                clear_table<kSlice>(a, list);
+                __syncthreads();
+            }
+            for (uint32_t j = threadIdx.x; j < a.k; j += kSlice) {
+                t_max = fmaxf(t_max, read_entry(a, p.r, j, list));
+                const int32_t at = list.at[j];
+                if (JOIN && at >= 0)
+                    list.z[j] = a.list_logits[(size_t)p.r * a.k + j];
+                if (in_part<DT>(a, p, at)) {
+                    if constexpr (!JOIN)
+                        list.z[j] = load_one<DT>(a.logits, z0 + (uint32_t)at);
+                    if (a.dlogits)
+                        enter(a, list, at);
+                }
+            }
+        }
+        group_reduce<Max, Max, W>(t_max, unused, red);
+        for (uint32_t j = threadIdx.x; j < a.k; j += kSlice)
+            if (list.at[j] >= 0)
+                t_sum += exp_of(a, list.t[j] - t_max);
+        group_reduce<Sum, Sum, W>(t_sum, unused, red + 2 * W);
+        const bool some = t_max != -INFINITY;
+        const float t_log = logf(t_sum), z_log = logf(z_sum), t_part = 1.f / t_sum;
+        float loss = 0.f;
+        for (uint32_t j = threadIdx.x; j < a.k; j += kSlice)
+            if (list.at[j] >= 0) {
+                const float t = list.t[j] - t_max, q = exp_of(a, t) * t_part;
+                if (JOIN && p.part == 0) {
+                    const float log_q = (list.z[j] - z_max) * a.per_t - z_log;
+                    loss += log_q == -INFINITY ? INFINITY : q * ((t * a.per_t - t_log) - log_q);
+                }
+                list.t[j] = q;
+            }
+        if (JOIN && p.part == 0) {
+            loss = lanes_reduce<Sum, 64>(loss);
+            if ((threadIdx.x & 63) == 0)
+                red[4 * W + (threadIdx.x >> 6)] = loss;
+        }
+        __syncthreads();
+        if (JOIN && p.part == 0 && threadIdx.x == 0) {
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; w++)
+                sum += red[4 * W + w];
+            a.loss[p.r] = some ? a.temperature * a.temperature * sum : 0.f;
+            if (a.row_max) {
+                a.row_max[p.r] = z_max;
+                a.row_sum[p.r] = z_sum;
+            }
+        }
+        if (a.dlogits) {
+            const float g = (a.row_weight ? a.row_weight[p.r] : 1.f) * a.temperature, g_q = g / z_sum;
+            const bool none = !some || g == 0.f;
+            const size_t d0 = p.r * a.ld_dlogits;
+            float v[N];
+            auto put = [&](u32x4 raw, size_t c, uint32_t left) {
+                unpack<DT>(raw, v);
+#pragma unroll
+                for (int e = 0; e < N; e++)
+                    v[e] = none ? 0.f : exp_of(a, v[e] - z_max) * g_q;
+                store_chunk<DT>(a.dlogits, d0 + c * N, left, pack<DT>(v));
+            };
+            for (uint32_t c0 = p.begin + threadIdx.x; c0 < p.end; c0 += P * kSlice) {
+                u32x4 raw[P];
+#pragma unroll
+                for (int i = 0; i < P; i++) {
+                    raw[i] = u32x4{0u, 0u, 0u, 0u};
+                    if (c0 + (uint32_t)i * kSlice < p.end)
+                        raw[i] = load_chunk<DT>(a.logits, z0 + (size_t)(c0 + (uint32_t)i * kSlice) * N, N);
+                }
+#pragma unroll
+                for (int i = 0; i < P; i++)
+                    if (c0 + (uint32_t)i * kSlice < p.end)
+                        put(raw[i], c0 + (uint32_t)i * kSlice, N);
+            }
+            if (a.tail && p.last && threadIdx.x == 0)
+                put(load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail), a.full, a.tail);
+            __syncthreads();
+            const bool repeats = a.k && *list.repeats != 0;
+            for (uint32_t j = threadIdx.x; j < a.k && !none; j += kSlice) {
+                const int32_t at = list.at[j];
+                if (in_part<DT>(a, p, at))
+                    store_one<DT>(a.dlogits, d0 + (uint32_t)at, exp_of(a, list.z[j] - z_max) * g_q - g * (repeats ? share_of(a, list, at) : list.t[j]));
+            }
+        }
+        if (id + gridDim.x < (uint64_t)a.rows * a.parts)
+            __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------------------------------------------------
+struct RowKernel {
+    uint32_t threads, chunks;                                                   // that the workgroup holds
+    void (*kernel[2])(const DistillArgs);
+};
+
+#define ROW_KERNEL(T, P) {T, T * P, {distill_row_kernel<kF32, T, P>, distill_row_kernel<kBF16, T, P>}}
+static const RowKernel kRowKernels[] = {ROW_KERNEL(64, 4), ROW_KERNEL(64, 16), ROW_KERNEL(256, 8), ROW_KERNEL(256, 16), ROW_KERNEL(512, 16), ROW_KERNEL(1024, 16)};
+#undef ROW_KERNEL
+constexpr uint32_t kHeld = 1024 * 16;
+
+// How a call is cut: parts = 0 is a row per workgroup.
+struct Cut {
+    uint32_t parts, part_chunks;
+};
+
+static Cut cut_rows(int64_t rows, uint32_t chunks, uint32_t least, uint32_t most)
+{
+    // about four workgroups on each of 256 compute units, parts of `least` ... `most` chunks
+    uint64_t parts = (1024 + rows - 1) / rows;
+    const uint64_t upper = (chunks + least - 1) / least, lower = (chunks + (uint64_t)most - 1) / most;
+    parts = parts > upper ? upper : parts;
+    parts = parts < lower ? lower : parts;
+    parts = parts > kMaxParts ? kMaxParts : parts < 1 ? 1 : parts;
+    uint32_t size = (uint32_t)((chunks + parts - 1) / parts);
+    size = size ? size : 1;
+    return {chunks ? (chunks + size - 1) / size : 1, size};
+}
+
+static Cut cut_loss(int64_t rows, int64_t vocab, tmask_dtype dt)
+{
+    const uint32_t chunks = (uint32_t)(vocab / (dt == TMASK_F32 ? 4 : 8));
+    if (chunks <= 1024 || (rows >= 256 && chunks <= kHeld))
+        return {0, 0};
+    return cut_rows(rows, chunks, 512, 4096);
+}
+
+static uint32_t grid_of(uint64_t workgroups) { return (uint32_t)(workgroups < (1u << 20) ? workgroups : 1u << 20); }
 
 // Everything but the outputs; `args` is complete when the result is TMASK_OK and rows > 0.
 static int check_distill(const tmask_distill_desc *desc, tmask_dtype dt, tmask_dtype teacher_dt, int index_bits, float temperature,
@@ -145,8 +504,8 @@ static int check_distill(const tmask_distill_desc *desc, tmask_dtype dt, tmask_d
     const tmask_distill_desc &d = *desc;
     if (!known(dt) || !known(teacher_dt) || (index_bits != 32 && index_bits != 64))
         return fail(TMASK_ERR_DTYPE, "unknown dtype %d, teacher's dtype %d or index of %d bits", (int)dt, (int)teacher_dt, index_bits);
-    if (!valid_sizes(d.rows, d.vocab) || d.k < 0 || d.k > kMaxEntries)
-        return fail(TMASK_ERR_SHAPE, "rows=%lld vocab=%lld k=%lld (at most %d)", (long long)d.rows, (long long)d.vocab, (long long)d.k, kMaxEntries);
+    if (!valid_sizes(d.rows, d.vocab) || d.k < 0 || d.k > (int64_t)kMaxEntries)
+        return fail(TMASK_ERR_SHAPE, "rows=%lld vocab=%lld k=%lld (at most %u)", (long long)d.rows, (long long)d.vocab, (long long)d.k, kMaxEntries);
     if (!(temperature > 0.f) || std::isinf(temperature))
         return fail(TMASK_ERR_SHAPE, "temperature=%g must be finite and positive", (double)temperature);
     if (d.rows == 0)
@@ -156,8 +515,20 @@ static int check_distill(const tmask_distill_desc *desc, tmask_dtype dt, tmask_d
     TMASK_TRY(check_rows("index", d.index, d.ld_index, d.rows, d.k, (size_t)index_bits / 8, d.k > 0));
     TMASK_TRY(check_vector("row_weight", d.row_weight, 4, false));
     TMASK_TRY(check_rows("dlogits", d.dlogits, d.ld_dlogits, d.rows, d.vocab, size_of(dt), false));
-    *args = DistillArgs{d.logits, d.teacher, d.index, d.row_weight, d.loss, d.row_max, d.row_sum, d.dlogits, (size_t)d.ld_logits,
-                        (size_t)d.ld_teacher, (size_t)d.ld_index, (size_t)d.ld_dlogits, (uint32_t)d.rows, (uint32_t)d.vocab, (uint32_t)d.k, temperature};
+    DistillArgs &a = *args;
+    a.logits = d.logits; a.teacher = d.teacher; a.index = d.index; a.row_weight = d.row_weight;
+    a.loss = d.loss; a.row_max = d.row_max; a.row_sum = d.row_sum; a.dlogits = d.dlogits;
+    a.part_stats = a.list_logits = nullptr;
+    a.ld_logits = (size_t)d.ld_logits; a.ld_teacher = (size_t)d.ld_teacher; a.ld_index = (size_t)d.ld_index; a.ld_dlogits = (size_t)d.ld_dlogits;
+    a.rows = (uint32_t)d.rows; a.vocab = (uint32_t)d.vocab; a.k = (uint32_t)d.k;
+    const uint32_t n = dt == TMASK_F32 ? 4 : 8;
+    a.full = a.vocab / n; a.tail = a.vocab % n;
+    a.parts = a.part_chunks = 0;
+    a.teacher_f32 = teacher_dt == TMASK_F32; a.index64 = index_bits == 64;
+    a.hash_shift = 31;
+    while (a.hash_shift > 0 && (1u << (32u - a.hash_shift)) < 2u * a.k)
+        a.hash_shift--;
+    a.temperature = temperature; a.per_t = 1.f / temperature; a.per_t2 = (float)(1.4426950408889634 / (double)temperature);
     return TMASK_OK;
 }
 
@@ -165,22 +536,23 @@ static int check_distill(const tmask_distill_desc *desc, tmask_dtype dt, tmask_d
 
 using namespace tmask;
 
-#define KERNELS(NAME)                                                              \
-    {{{NAME<kF32, kF32, 32>, NAME<kF32, kF32, 64>}, {NAME<kF32, kBF16, 32>, NAME<kF32, kBF16, 64>}}, \
-     {{NAME<kBF16, kF32, 32>, NAME<kBF16, kF32, 64>}, {NAME<kBF16, kBF16, 32>, NAME<kBF16, kBF16, 64>}}}
-
+// Sizes that take parts need, for both types, room for the statistics of every part and a list's logits for every row.
 extern "C" size_t tmask_distill_workspace_bytes(int64_t rows, int64_t vocab)
 {
-    (void)rows;
-    (void)vocab;
-    return 0;
+    if (!valid_sizes(rows, vocab) || rows == 0)
+        return 0;
+    size_t most = 0;
+    for (const tmask_dtype dt : {TMASK_F32, TMASK_BF16}) {
+        const size_t parts = cut_loss(rows, vocab, dt).parts;
+        const size_t need = parts ? (size_t)rows * (2u * parts + kMaxEntries) * 4u : 0;
+        most = need > most ? need : most;
+    }
+    return most;
 }
 
 extern "C" int tmask_distill(const tmask_distill_desc *desc, tmask_dtype dt, tmask_dtype teacher_dt, int index_bits, float temperature,
                              void *workspace, size_t workspace_bytes, void *hip_stream)
 {
-    (void)workspace;
-    (void)workspace_bytes;
     DistillArgs a;
     TMASK_TRY(check_distill(desc, dt, teacher_dt, index_bits, temperature, &a));
     if (desc->rows == 0)
@@ -188,8 +560,26 @@ extern "C" int tmask_distill(const tmask_distill_desc *desc, tmask_dtype dt, tma
     TMASK_TRY(check_vector("loss", desc->loss, 4, true));
     TMASK_TRY(check_vector("row_max", desc->row_max, 4, desc->row_sum != nullptr));
     TMASK_TRY(check_vector("row_sum", desc->row_sum, 4, desc->row_max != nullptr));
-    static void (*const kernels[2][2][2])(const DistillArgs) = KERNELS(distill_kernel);
-    hipLaunchKernelGGL(kernels[dt][teacher_dt][index_bits == 64], dim3(a.rows < 65536 ? a.rows : 65536), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
+    hipStream_t stream = (hipStream_t)hip_stream;
+    const Cut cut = cut_loss(desc->rows, desc->vocab, dt);
+    const size_t list = list_bytes(a.k, a.hash_shift);
+    const bool bf16 = dt == TMASK_BF16;
+    if (cut.parts == 0) {
+        const RowKernel *k = kRowKernels;
+        while (k->chunks < a.full)
+            k++;
+        hipLaunchKernelGGL(k->kernel[bf16], dim3(grid_of(a.rows)), dim3(k->threads), 20 * (k->threads / 64) + list, stream, a);
+    } else {
+        TMASK_TRY(check_workspace(workspace, workspace_bytes, tmask_distill_workspace_bytes(desc->rows, desc->vocab)));
+        a.parts = cut.parts;
+        a.part_chunks = cut.part_chunks;
+        a.part_stats = (float *)workspace;
+        a.list_logits = a.part_stats + (size_t)a.rows * a.parts * 2u;
+        const uint32_t grid = grid_of((uint64_t)a.rows * a.parts);
+        hipLaunchKernelGGL(bf16 ? distill_part_kernel<kBF16> : distill_part_kernel<kF32>, dim3(grid), dim3(kSlice), 0, stream, a);
+        hipLaunchKernelGGL((bf16 ? distill_slice_kernel<kBF16, true> : distill_slice_kernel<kF32, true>), dim3(grid), dim3(kSlice),
+                           20 * (kSlice / 64) + list, stream, a);
+    }
     return launched("distillation launch");
 }
 
@@ -203,7 +593,10 @@ extern "C" int tmask_distill_backward(const tmask_distill_desc *desc, tmask_dtyp
     TMASK_TRY(check_vector("row_max", desc->row_max, 4, true));
     TMASK_TRY(check_vector("row_sum", desc->row_sum, 4, true));
     TMASK_TRY(check_rows("dlogits", desc->dlogits, desc->ld_dlogits, desc->rows, desc->vocab, size_of(dt), true));
-    static void (*const kernels[2][2][2])(const DistillArgs) = KERNELS(distill_grad_kernel);
-    hipLaunchKernelGGL(kernels[dt][teacher_dt][index_bits == 64], dim3(a.rows < 65536 ? a.rows : 65536), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
+    const Cut cut = cut_rows(desc->rows, a.full, 512, 8192);
+    a.parts = cut.parts;
+    a.part_chunks = cut.part_chunks;
+    hipLaunchKernelGGL((dt == TMASK_BF16 ? distill_slice_kernel<kBF16, false> : distill_slice_kernel<kF32, false>),
+                       dim3(grid_of((uint64_t)a.rows * a.parts)), dim3(kSlice), 20 * (kSlice / 64) + list_bytes(a.k, a.hash_shift), (hipStream_t)hip_stream, a);
     return launched("distillation gradient launch");
 }

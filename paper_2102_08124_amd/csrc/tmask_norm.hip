@@ -12,6 +12,22 @@
 
 namespace tmask {
 
+// sum over the workgroup, in every thread; `red` has a place for each wavefront and may be used again at once
+template <int WAVES>
+__device__ __forceinline__ float group_sum(float v, float *red)
+{
+    v = lanes_reduce<Sum, 64>(v);
+    if ((threadIdx.x & 63) == 0)
+        red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; w++)
+        v += red[w];
+    __syncthreads();
+    return v;
+}
+
 struct NormArgs {
     const void *x, *residual, *weight, *bias;
     void *y, *total;

@@ -1,8 +1,18 @@
-// What the row kernels (layer norm, bias + GELU, distillation) share: elements of both types as fp32, sums over a workgroup.
+// What the row kernels (layer norm, bias + GELU, distillation) share: rows in chunks of 16 bytes, sums over lanes and workgroups.
 #pragma once
 #include "tmask_device.hpp"
 
 namespace tmask {
+
+// A chunk may begin at any element: 16-byte loads and stores work at any address, at somewhat less speed than at multiples of 16.
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+
+template <int DT>
+constexpr int kElems = DT == kF32 ? 4 : 8;          // of a chunk
+
+template <int DT>
+constexpr int kSize = DT == kF32 ? 4 : 2;           // bytes of an element
 
 // element i of an array of type DT, as fp32
 template <int DT>
@@ -24,43 +34,143 @@ __device__ __forceinline__ void store_one(void *p, size_t i, float v)
         ((__bf16 *)p)[i] = (__bf16)v;
 }
 
-// sum over the workgroup, in every thread; `red` has a place for each wavefront and may be used again at once
-template <int WAVES>
-__device__ __forceinline__ float group_sum(float v, float *red)
+// elements i ... of an array, of which `left` belong to the row (at least one); the others are `fill`, a value of the type
+template <int DT>
+__device__ __forceinline__ u32x4 load_chunk(const void *p, size_t i, uint32_t left, float fill = 0.f)
 {
+    const unsigned char *const a = (const unsigned char *)p + i * kSize<DT>;
+    if (left >= (uint32_t)kElems<DT>) {
+        if constexpr (DT == kF32)
+            return *(const u32x4_at4 *)a;
+        else
+            return *(const u32x4_at2 *)a;
+    }
+    u32x4 v;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-        v += __shfl_xor(v, d, 64);
-    if constexpr (WAVES > 1) {
-        if ((threadIdx.x & 63) == 0)
-            red[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0.f;
-#pragma unroll
-        for (int w = 0; w < WAVES; w++)
-            v += red[w];
-        __syncthreads();
+    for (int e = 0; e < 4; e++) {
+        const uint32_t f = __float_as_uint(fill);
+        if constexpr (DT == kF32) {
+            v[e] = (uint32_t)e < left ? ((const uint32_t *)a)[e] : f;
+        } else {
+            const uint32_t lo = 2u * e < left ? ((const uint16_t *)a)[2 * e] : f >> 16, hi = 2u * e + 1u < left ? ((const uint16_t *)a)[2 * e + 1] : f >> 16;
+            v[e] = lo | hi << 16;
+        }
     }
     return v;
 }
 
-template <int WAVES>
-__device__ __forceinline__ float group_max(float v, float *red)
+template <int DT>
+__device__ __forceinline__ void unpack(u32x4 raw, float (&v)[kElems<DT>])
 {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-        v = fmaxf(v, __shfl_xor(v, d, 64));
-    if constexpr (WAVES > 1) {
-        if ((threadIdx.x & 63) == 0)
-            red[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = red[0];
+    for (int e = 0; e < 4; e++)
+        if constexpr (DT == kF32) {
+            v[e] = __uint_as_float(raw[e]);
+        } else {
+            v[2 * e] = __uint_as_float(raw[e] << 16);
+            v[2 * e + 1] = __uint_as_float(raw[e] & 0xFFFF0000u);
+        }
+}
+
+// rounded to nearest even, by the hardware's packed conversion
+template <int DT>
+__device__ __forceinline__ u32x4 pack(const float (&v)[kElems<DT>])
+{
+    u32x4 raw;
 #pragma unroll
-        for (int w = 1; w < WAVES; w++)
-            v = fmaxf(v, red[w]);
-        __syncthreads();
+    for (int e = 0; e < 4; e++)
+        if constexpr (DT == kF32) {
+            raw[e] = __float_as_uint(v[e]);
+        } else {
+            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
+            raw[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e], v[2 * e + 1]}, bf16x2));
+        }
+    return raw;
+}
+
+template <int DT>
+__device__ __forceinline__ void store_chunk(void *p, size_t i, uint32_t left, u32x4 raw)
+{
+    unsigned char *const a = (unsigned char *)p + i * kSize<DT>;
+    if (left >= (uint32_t)kElems<DT>) {
+        if constexpr (DT == kF32)
+            *(u32x4_at4 *)a = raw;
+        else
+            *(u32x4_at2 *)a = raw;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        if constexpr (DT == kF32) {
+            if ((uint32_t)e < left)
+                ((uint32_t *)a)[e] = raw[e];
+        } else {
+            if (2u * e < left)
+                ((uint16_t *)a)[2 * e] = (uint16_t)raw[e];
+            if (2u * e + 1u < left)
+                ((uint16_t *)a)[2 * e + 1] = (uint16_t)(raw[e] >> 16);
+        }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Sums and maxima over LANES neighbouring lanes, in every one of them and with the same bits: each step adds a lane's number to
+// that of its mirror image in a group twice as large, by DPP up to 16 lanes and by the half-exchanges of gfx950 above.
+// ---------------------------------------------------------------------------------------------------------------------
+struct Sum {
+    static __device__ __forceinline__ float of(float a, float b) { return a + b; }
+};
+struct Max {
+    static __device__ __forceinline__ float of(float a, float b) { return fmaxf(a, b); }
+};
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, false));
+}
+
+template <typename Op, int LANES>
+__device__ __forceinline__ float lanes_reduce(float v)
+{
+    static_assert(LANES == 8 || LANES == 16 || LANES == 32 || LANES == 64, "lanes");
+    v = Op::of(v, dpp<0xB1>(v));                    // quad: neighbours
+    v = Op::of(v, dpp<0x4E>(v));                    // quad: pairs
+    v = Op::of(v, dpp<0x141>(v));                   // half rows of 8 mirrored
+    if constexpr (LANES >= 16)
+        v = Op::of(v, dpp<0x140>(v));               // rows of 16 mirrored
+    if constexpr (LANES >= 32) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = Op::of(__uint_as_float(s[0]), __uint_as_float(s[1]));
+    }
+    if constexpr (LANES >= 64) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = Op::of(__uint_as_float(s[0]), __uint_as_float(s[1]));
     }
     return v;
+}
+
+// Two numbers over a workgroup of WAVES wavefronts, in every thread.  `red`: 2 WAVES numbers of LDS that nothing else uses between
+// the barrier before this call and the one after the next: calls in a row take turns with two such places.
+template <typename OpA, typename OpB, int WAVES>
+__device__ __forceinline__ void group_reduce(float &a, float &b, float *red)
+{
+    a = lanes_reduce<OpA, 64>(a);
+    b = lanes_reduce<OpB, 64>(b);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) {
+            red[threadIdx.x >> 6] = a;
+            red[WAVES + (threadIdx.x >> 6)] = b;
+        }
+        __syncthreads();
+        a = red[0];
+        b = red[WAVES];
+#pragma unroll
+        for (int w = 1; w < WAVES; w++) {
+            a = OpA::of(a, red[w]);
+            b = OpB::of(b, red[WAVES + w]);
+        }
+    }
 }
 
 }  // namespace tmask
