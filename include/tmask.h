@@ -346,7 +346,7 @@ int tmask_nm_sparse_probability(int N, int M, double rho, double *prob);
  * A sparse model is trained, or recovered from its dense teacher, by steps whose products tmask_spmm24 computes; the
  * calls below are what such a step does between them, forward and backward, and its loss.  They work on rows of any width:
  * rows >= 0, cols > 0 (rows = 0: nothing is done, and column sums are 0), every leading dimension >= the row's width and
- * < 2^31 (it does not matter for a single row), rows and cols < 2^31, pointers aligned to their element type.  Any such layout
+ * < 2^31 (it does not matter for a single row), rows < 2^31, cols at most 2^28 (vocab < 2^31), pointers aligned to their element type.  Any such layout
  * is taken; rows that begin at multiples of 16 bytes are read fastest.  `dt` is the type of activations and logits and of
  * their gradients, `param_dt` that of weight, bias and their gradients.  All arithmetic is in fp32 and rounded once, to nearest
  * even, where a result is stored; sums are added up in an order that depends on the sizes alone, so the same call gives the same

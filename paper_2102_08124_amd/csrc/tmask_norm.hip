@@ -12,81 +12,254 @@
 
 namespace tmask {
 
-// sum over the workgroup, in every thread; `red` has a place for each wavefront and may be used again at once
-template <int WAVES>
-__device__ __forceinline__ float group_sum(float v, float *red)
-{
-    v = lanes_reduce<Sum, 64>(v);
-    if ((threadIdx.x & 63) == 0)
-        red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.f;
-#pragma unroll
-    for (int w = 0; w < WAVES; w++)
-        v += red[w];
-    __syncthreads();
-    return v;
-}
-
 struct NormArgs {
     const void *x, *residual, *weight, *bias;
     void *y, *total;
     float *mean, *rstd;
     size_t ld_x, ld_residual, ld_y, ld_total;
     uint32_t rows, cols;
-    float eps;
+    uint32_t param_f32;
+    float eps, per_col;                   // 1 / cols
 };
 
 struct NormGradArgs {
     const void *dy, *x, *weight, *dtotal;
     const float *mean, *rstd;
     void *dx;
-    float *partial;                       // strips x {dweight, dbias} x cols
+    void *dweight, *dbias;
+    float *partial;                       // strips x {dweight, dbias} x pitch
     size_t ld_dy, ld_x, ld_dtotal, ld_dx;
-    uint32_t rows, cols, strips;
+    uint32_t rows, cols;
+    uint32_t param_f32;
+    uint32_t strips, pitch;               // strips = 1: the sums go straight to dweight and dbias
+    float per_col;
 };
 
 struct GeluArgs {
     const void *dy, *x, *bias;            // dy: gradients
-    void *out;
-    float *partial;                       // strips x cols
+    void *out, *dbias;
+    float *partial;                       // strips x pitch
     size_t ld_dy, ld_x, ld_out;
-    uint32_t rows, cols, strips;
+    uint32_t rows, cols, chunks;          // chunks of a row, the last of them perhaps cut
+    uint32_t param_f32;
+    uint32_t lanes_log2;                  // lanes of a workgroup that share a row
+    uint32_t groups, strips, pitch;       // workgroups beside each other, and below
 };
 
 struct ColumnArgs {
-    const float *partial;                 // strips x (sums x cols)
+    const float *partial;                 // strips x sums x pitch
     void *out[2];
-    uint32_t cols, strips, sums;
+    uint32_t cols, strips, sums, pitch;
+    uint32_t param_f32;
 };
 
-template <int DT, int PDT>
-__global__ void __launch_bounds__(kThreads) norm_kernel(const NormArgs p)
+__device__ __forceinline__ float load_param(const void *p, uint32_t f32, size_t i) { return f32 ? load_one<kF32>(p, i) : load_one<kBF16>(p, i); }
+
+__device__ __forceinline__ void store_param(void *p, uint32_t f32, size_t i, float v)
 {
-    __shared__ float red[kThreads / 64];
+    if (f32)
+        store_one<kF32>(p, i, v);
+    else
+        store_one<kBF16>(p, i, v);
+}
+
+// N parameters from column c on, of which `left` exist
+template <int N>
+__device__ __forceinline__ void load_params(const void *p, uint32_t f32, size_t c, uint32_t left, float (&v)[N])
+{
+    if (f32) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4)
+            if ((uint32_t)e < left) {
+                float four[4];
+                unpack<kF32>(load_chunk<kF32>(p, c + e, left - e), four);
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    v[e + i] = four[i];
+            }
+    } else if constexpr (N % 8 == 0) {
+#pragma unroll
+        for (int e = 0; e < N; e += 8)
+            if ((uint32_t)e < left) {
+                float eight[8];
+                unpack<kBF16>(load_chunk<kBF16>(p, c + e, left - e), eight);
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    v[e + i] = eight[i];
+            }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            if ((uint32_t)e < left)
+                v[e] = load_one<kBF16>(p, c + e);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Layer norm of rows that stay in registers: LANES lanes (a part of a wavefront, or a workgroup of several) with E elements each,
+// in chunks of 16 bytes that alternate between the lanes.  The mean first, then the mean of the squared differences
+// from it: both from registers, so that a large mean costs no digits and nothing is read twice.
+// ---------------------------------------------------------------------------------------------------------------------
+template <int LANES>
+constexpr int kNormThreads = LANES <= 256 ? 256 : LANES;
+
+template <int LANES, int T>
+__device__ __forceinline__ float row_sum(float v, float *red)
+{
+    v = lanes_reduce<Sum, LANES < 64 ? LANES : 64>(v);
+    if constexpr (LANES > 64) {
+        constexpr int W = T / 64;
+        static_assert(LANES == T, "a row has the whole workgroup");
+        if ((threadIdx.x & 63) == 0)
+            red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = red[0];
+#pragma unroll
+        for (int w = 1; w < W; w++)
+            v += red[w];
+    }
+    return v;
+}
+
+template <int DT, int LANES, int E>
+__global__ void __launch_bounds__(kNormThreads<LANES>) norm_kernel(const NormArgs p)
+{
+    constexpr int T = kNormThreads<LANES>, N = kElems<DT>, C = E / N, kRows = T / LANES;
+    __shared__ float red[2][LANES > 64 ? T / 64 : 1];
+    const uint32_t lane = threadIdx.x % LANES;
+    float w[E], b[E];
+    uint32_t left[C];
+#pragma unroll
+    for (int i = 0; i < C; i++) {
+        const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
+        left[i] = c >= p.cols ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
+        float v[N];
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            v[e] = 1.f;
+        if (p.weight && left[i])
+            load_params<N>(p.weight, p.param_f32, c, left[i], v);
+#pragma unroll
+        for (int e = 0; e < N; e++) {
+            w[i * N + e] = v[e];
+            v[e] = 0.f;
+        }
+        if (p.bias && left[i])
+            load_params<N>(p.bias, p.param_f32, c, left[i], v);
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            b[i * N + e] = v[e];
+    }
+    const bool whole = p.cols == (uint32_t)(LANES * E);
+    for (uint32_t r = blockIdx.x * kRows + threadIdx.x / LANES; r < p.rows; r += gridDim.x * kRows) {
+        u32x4 raw[C], more[C];
+#pragma unroll
+        for (int i = 0; i < C; i++) {
+            const size_t c = (lane + (uint32_t)(i * LANES)) * N;
+            raw[i] = more[i] = u32x4{0u, 0u, 0u, 0u};
+            if (left[i]) {
+                raw[i] = load_chunk<DT>(p.x, r * p.ld_x + c, left[i]);
+                if (p.residual)
+                    more[i] = load_chunk<DT>(p.residual, r * p.ld_residual + c, left[i]);
+            }
+        }
+        float t[E], s = 0.f;
+#pragma unroll
+        for (int i = 0; i < C; i++) {
+            float v[N], u[N];
+            unpack<DT>(raw[i], v);
+            unpack<DT>(more[i], u);
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                v[e] += u[e];
+                t[i * N + e] = v[e];
+                s += v[e];
+            }
+            if (p.total && left[i])
+                store_chunk<DT>(p.total, r * p.ld_total + (size_t)(lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
+        }
+        const float mean = row_sum<LANES, T>(s, red[0]) * p.per_col;
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < C; i++)
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                const float d = whole || (uint32_t)e < left[i] ? t[i * N + e] - mean : 0.f;
+                t[i * N + e] = d;
+                s += d * d;
+            }
+        const float rstd = 1.f / sqrtf(row_sum<LANES, T>(s, red[1]) * p.per_col + p.eps);
+#pragma unroll
+        for (int i = 0; i < C; i++) {
+            float v[N];
+#pragma unroll
+            for (int e = 0; e < N; e++)
+                v[e] = t[i * N + e] * rstd * w[i * N + e] + b[i * N + e];
+            if (left[i])
+                store_chunk<DT>(p.y, r * p.ld_y + (size_t)(lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
+        }
+        if (p.mean && lane == 0) {
+            p.mean[r] = mean;
+            p.rstd[r] = rstd;
+        }
+    }
+}
+
+// Rows that no workgroup holds: three passes, the second and third through the caches.
+constexpr int kLongThreads = 1024;
+
+template <int DT>
+__global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormArgs p)
+{
+    constexpr int N = kElems<DT>;
+    __shared__ float red[2][kLongThreads / 64];
     for (uint32_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
-        const size_t x0 = r * p.ld_x, r0 = r * p.ld_residual;
-        auto total = [&](uint32_t c) {
-            const float v = load_one<DT>(p.x, x0 + c);
-            return p.residual ? v + load_one<DT>(p.residual, r0 + c) : v;
+        auto each = [&](auto f) {
+            for (uint32_t c = threadIdx.x * N; c < p.cols; c += kLongThreads * N) {
+                const uint32_t left = p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
+                float v[N], u[N];
+                unpack<DT>(load_chunk<DT>(p.x, r * p.ld_x + c, left), v);
+                if (p.residual) {
+                    unpack<DT>(load_chunk<DT>(p.residual, r * p.ld_residual + c, left), u);
+#pragma unroll
+                    for (int e = 0; e < N; e++)
+                        v[e] += u[e];
+                }
+                f(c, left, v);
+            }
         };
         float s = 0.f;
-        for (uint32_t c = threadIdx.x; c < p.cols; c += kThreads)
-            s += total(c);
-        const float mean = group_sum<kThreads / 64>(s, red) / (float)p.cols;
+        each([&](uint32_t, uint32_t, float (&v)[N]) {
+#pragma unroll
+            for (int e = 0; e < N; e++)
+                s += v[e];
+        });
+        const float mean = row_sum<kLongThreads, kLongThreads>(s, red[0]) * p.per_col;
         s = 0.f;
-        for (uint32_t c = threadIdx.x; c < p.cols; c += kThreads) {
-            const float d = total(c) - mean;
-            s += d * d;
-        }
-        const float rstd = 1.f / sqrtf(group_sum<kThreads / 64>(s, red) / (float)p.cols + p.eps);
-        for (uint32_t c = threadIdx.x; c < p.cols; c += kThreads) {
-            const float t = total(c);
-            const float w = p.weight ? load_one<PDT>(p.weight, c) : 1.f, b = p.bias ? load_one<PDT>(p.bias, c) : 0.f;
+        each([&](uint32_t, uint32_t left, float (&v)[N]) {
+#pragma unroll
+            for (int e = 0; e < N; e++)
+                s += (uint32_t)e < left ? (v[e] - mean) * (v[e] - mean) : 0.f;
+        });
+        const float rstd = 1.f / sqrtf(row_sum<kLongThreads, kLongThreads>(s, red[1]) * p.per_col + p.eps);
+        each([&](uint32_t c, uint32_t left, float (&v)[N]) {
+            float w[N], b[N];
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                w[e] = 1.f;
+                b[e] = 0.f;
+            }
+            if (p.weight)
+                load_params<N>(p.weight, p.param_f32, c, left, w);
+            if (p.bias)
+                load_params<N>(p.bias, p.param_f32, c, left, b);
             if (p.total)
-                store_one<DT>(p.total, r * p.ld_total + c, t);
-            store_one<DT>(p.y, r * p.ld_y + c, (t - mean) * rstd * w + b);
-        }
+                store_chunk<DT>(p.total, r * p.ld_total + c, left, pack<DT>(v));
+#pragma unroll
+            for (int e = 0; e < N; e++)
+                v[e] = (v[e] - mean) * rstd * w[e] + b[e];
+            store_chunk<DT>(p.y, r * p.ld_y + c, left, pack<DT>(v));
+        });
         if (p.mean && threadIdx.x == 0) {
             p.mean[r] = mean;
             p.rstd[r] = rstd;
@@ -94,32 +267,168 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const NormArgs p)
     }
 }
 
-template <int DT, int PDT>
-__global__ void __launch_bounds__(kThreads) norm_grad_kernel(const NormGradArgs p)
+// ---------------------------------------------------------------------------------------------------------------------
+// Its gradients, with rows held the same way.  A workgroup goes through every strips-th group of rows and keeps the sums over
+// them of dy h and dy in registers, a column in the same lane all the time; at its end the lanes and wavefronts that share
+// a column add up in LDS, and the strips' sums are added up by columns_kernel.  Rows are loaded one ahead.
+// ---------------------------------------------------------------------------------------------------------------------
+template <int LANES>
+constexpr int kNormGradThreads = LANES <= 64 ? 512 : LANES;
+
+// `v` over the lanes of a wavefront with the same number modulo LANES
+template <int LANES>
+__device__ __forceinline__ float across_rows(float v)
 {
-    __shared__ float red[kThreads / 64];
-    for (uint32_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
-        const float mean = p.mean[r], rstd = p.rstd[r];
-        float s1 = 0.f, s2 = 0.f;
-        for (uint32_t c = threadIdx.x; c < p.cols; c += kThreads) {
-            const float d = load_one<DT>(p.dy, r * p.ld_dy + c) * (p.weight ? load_one<PDT>(p.weight, c) : 1.f);
-            s1 += d;
-            s2 += d * ((load_one<DT>(p.x, r * p.ld_x + c) - mean) * rstd);
+    if constexpr (LANES <= 8)
+        v += dpp<0x128>(v);                         // rows of 16 rotated by 8
+    if constexpr (LANES <= 16) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    if constexpr (LANES <= 32) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    return v;
+}
+
+template <int DT, int LANES, int E>
+__global__ void __launch_bounds__(kNormGradThreads<LANES>) norm_grad_kernel(const NormGradArgs p)
+{
+    constexpr int T = kNormGradThreads<LANES>, N = kElems<DT>, C = E / N, kRows = T / LANES, W = T / 64, kCols = LANES * E;
+    __shared__ float red[2][2 * W];
+    const uint32_t lane = threadIdx.x % LANES;
+    float w[E], dw[E], db[E];
+    uint32_t left[C];
+#pragma unroll
+    for (int i = 0; i < C; i++) {
+        const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
+        left[i] = c >= p.cols ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
+        float v[N];
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            v[e] = 1.f;
+        if (p.weight && left[i])
+            load_params<N>(p.weight, p.param_f32, c, left[i], v);
+#pragma unroll
+        for (int e = 0; e < N; e++) {
+            w[i * N + e] = v[e];
+            dw[i * N + e] = db[i * N + e] = 0.f;
         }
-        s1 = group_sum<kThreads / 64>(s1, red) / (float)p.cols;
-        s2 = group_sum<kThreads / 64>(s2, red) / (float)p.cols;
-        for (uint32_t c = threadIdx.x; c < p.cols; c += kThreads) {
-            const float d = load_one<DT>(p.dy, r * p.ld_dy + c) * (p.weight ? load_one<PDT>(p.weight, c) : 1.f);
-            float v = rstd * (d - s1 - (load_one<DT>(p.x, r * p.ld_x + c) - mean) * rstd * s2);
-            if (p.dtotal)
-                v += load_one<DT>(p.dtotal, r * p.ld_dtotal + c);
-            store_one<DT>(p.dx, r * p.ld_dx + c, v);
+    }
+    struct Row {
+        u32x4 dy[C], x[C], more[C];
+        float mean, rstd;
+    } next;
+    auto fetch = [&](uint32_t r, Row &row) {
+#pragma unroll
+        for (int i = 0; i < C; i++) {
+            const size_t c = (lane + (uint32_t)(i * LANES)) * N;
+            row.dy[i] = row.x[i] = row.more[i] = u32x4{0u, 0u, 0u, 0u};
+            if (left[i] && r < p.rows) {
+                row.dy[i] = load_chunk<DT>(p.dy, r * p.ld_dy + c, left[i]);
+                row.x[i] = load_chunk<DT>(p.x, r * p.ld_x + c, left[i]);
+                if (p.dtotal)
+                    row.more[i] = load_chunk<DT>(p.dtotal, r * p.ld_dtotal + c, left[i]);
+            }
+        }
+        row.mean = r < p.rows ? p.mean[r] : 0.f;
+        row.rstd = r < p.rows ? p.rstd[r] : 0.f;
+    };
+    // the same number of rounds for the whole workgroup: barriers are inside
+    const uint32_t step = p.strips * kRows;
+    uint32_t r = blockIdx.x * kRows + threadIdx.x / LANES, turn = 0;
+    fetch(r, next);
+    for (uint32_t r0 = blockIdx.x * kRows; r0 < p.rows; r0 += step, r += step, turn ^= 1) {
+        const Row row = next;
+        if (r0 + step < p.rows)
+            fetch(r + step, next);
+        const bool exists = r < p.rows;
+        float d[E], h[E], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < C; i++) {
+            float v[N], u[N];
+            unpack<DT>(row.dy[i], v);
+            unpack<DT>(row.x[i], u);
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                const int k = i * N + e;
+                // dy is 0 in columns and rows that do not exist
+                h[k] = (u[e] - row.mean) * row.rstd;
+                dw[k] += v[e] * h[k];
+                db[k] += v[e];
+                d[k] = v[e] * w[k];
+                s1 += d[k];
+                s2 += d[k] * h[k];
+            }
+        }
+        if constexpr (LANES <= 64) {
+            s1 = lanes_reduce<Sum, LANES>(s1);
+            s2 = lanes_reduce<Sum, LANES>(s2);
+        } else {
+            group_reduce<Sum, Sum, W>(s1, s2, red[turn]);
+        }
+        s1 *= p.per_col;
+        s2 *= p.per_col;
+#pragma unroll
+        for (int i = 0; i < C; i++) {
+            float v[N];
+            unpack<DT>(row.more[i], v);
+#pragma unroll
+            for (int e = 0; e < N; e++)
+                v[e] += row.rstd * (d[i * N + e] - s1 - h[i * N + e] * s2);
+            if (left[i] && exists)
+                store_chunk<DT>(p.dx, r * p.ld_dx + (size_t)(lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
+        }
+    }
+    if (!p.dweight && !p.dbias)
+        return;
+    // (-0, not 0, would be the neutral element of these sums: a sum of no rows but of -0 alone ends as 0)
+    auto put = [&](uint32_t which, uint32_t c, float v) {
+        if (p.strips > 1) {
+            p.partial[((size_t)blockIdx.x * 2 + which) * p.pitch + c] = v;
+        } else {
+            void *const out = which ? p.dbias : p.dweight;
+            if (out)
+                store_param(out, p.param_f32, c, v);
+        }
+    };
+    if constexpr (kRows == 1) {
+#pragma unroll
+        for (int k = 0; k < E; k++) {
+            const uint32_t c = (lane + (uint32_t)(k / N * LANES)) * N + (uint32_t)(k % N);
+            if (c < p.cols) {
+                put(0, c, dw[k]);
+                put(1, c, db[k]);
+            }
+        }
+    } else {
+        __shared__ float sums[W][2][kCols];
+#pragma unroll
+        for (int k = 0; k < E; k++) {
+            const float a = across_rows<LANES>(dw[k]), b = across_rows<LANES>(db[k]);
+            const uint32_t c = (lane + (uint32_t)(k / N * LANES)) * N + (uint32_t)(k % N);
+            if ((threadIdx.x & 63) < (uint32_t)LANES) {
+                sums[threadIdx.x >> 6][0][c] = a;
+                sums[threadIdx.x >> 6][1][c] = b;
+            }
+        }
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < 2u * kCols; i += T) {
+            const uint32_t which = i / kCols, c = i % kCols;
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < W; k++)
+                s += sums[k][which][c];
+            if (c < p.cols)
+                put(which, c, s);
         }
     }
 }
 
+// Rows that no workgroup holds: the sums over rows first (dx may lie over dy or x), a column a thread, then dx in two passes.
 template <int DT>
-__global__ void __launch_bounds__(kThreads) norm_columns_kernel(const NormGradArgs p)
+__global__ void __launch_bounds__(kThreads) norm_long_columns_kernel(const NormGradArgs p)
 {
     const uint32_t c = blockIdx.x * kThreads + threadIdx.x;
     if (c >= p.cols)
@@ -130,84 +439,266 @@ __global__ void __launch_bounds__(kThreads) norm_columns_kernel(const NormGradAr
         db += dy;
         dw += dy * ((load_one<DT>(p.x, r * p.ld_x + c) - p.mean[r]) * p.rstd[r]);
     }
-    float *const out = p.partial + (size_t)blockIdx.y * 2u * p.cols + c;
+    float *const out = p.partial + (size_t)blockIdx.y * 2u * p.pitch + c;
     out[0] = dw;
-    out[p.cols] = db;
+    out[p.pitch] = db;
 }
 
-// u / 2 * (1 + erf(u / sqrt 2)) and its form with tanh, or the derivative
+template <int DT>
+__global__ void __launch_bounds__(kLongThreads) norm_long_grad_kernel(const NormGradArgs p)
+{
+    constexpr int N = kElems<DT>;
+    __shared__ float red[2][2 * kLongThreads / 64];
+    uint32_t turn = 0;
+    for (uint32_t r = blockIdx.x; r < p.rows; r += gridDim.x, turn ^= 1) {
+        const float mean = p.mean[r], rstd = p.rstd[r];
+        auto each = [&](auto f) {
+            for (uint32_t c = threadIdx.x * N; c < p.cols; c += kLongThreads * N) {
+                const uint32_t left = p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
+                float d[N], h[N], w[N];
+                unpack<DT>(load_chunk<DT>(p.dy, r * p.ld_dy + c, left), d);
+                unpack<DT>(load_chunk<DT>(p.x, r * p.ld_x + c, left), h);
+#pragma unroll
+                for (int e = 0; e < N; e++)
+                    w[e] = 1.f;
+                if (p.weight)
+                    load_params<N>(p.weight, p.param_f32, c, left, w);
+#pragma unroll
+                for (int e = 0; e < N; e++) {
+                    d[e] *= w[e];
+                    h[e] = (h[e] - mean) * rstd;
+                }
+                f(c, left, d, h);
+            }
+        };
+        float s1 = 0.f, s2 = 0.f;
+        each([&](uint32_t, uint32_t, float (&d)[N], float (&h)[N]) {
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                s1 += d[e];                                                     // d is 0 beyond the row
+                s2 += d[e] * h[e];
+            }
+        });
+        group_reduce<Sum, Sum, kLongThreads / 64>(s1, s2, red[turn]);
+        s1 *= p.per_col;
+        s2 *= p.per_col;
+        each([&](uint32_t c, uint32_t left, float (&d)[N], float (&h)[N]) {
+            float v[N];
+#pragma unroll
+            for (int e = 0; e < N; e++)
+                v[e] = 0.f;
+            if (p.dtotal)
+                unpack<DT>(load_chunk<DT>(p.dtotal, r * p.ld_dtotal + c, left), v);
+#pragma unroll
+            for (int e = 0; e < N; e++)
+                v[e] += rstd * (d[e] - s1 - h[e] * s2);
+            store_chunk<DT>(p.dx, r * p.ld_dx + c, left, pack<DT>(v));
+        });
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// GELU.  With E(a) = exp(-a^2 / 2), the share Phi(u) = (1 + erf(u / sqrt 2)) / 2 that passes is E(u) R(t) for u < 0 and one minus that of -u for
+// u > 0, t = 1 / (1 + 0.33 |u|): R is the polynomial of degree 5 without constant term for which E R differs least from
+// the share over all u (by 4.2e-8, fitted by linear programming; 1.8e-7 with the roundings of fp32).  The derivative Phi(u) + u E(u) / sqrt(2 pi) has the same exponential.  The form with
+// tanh is the share 1 / (1 + exp(-2 s)).
+// ---------------------------------------------------------------------------------------------------------------------
 template <int FORM, bool GRAD>
 __device__ __forceinline__ float gelu(float u)
 {
     if constexpr (FORM == TMASK_GELU_ERF) {
-        const float share = 0.5f * (1.f + erff(u * 0.70710678f));
-        return GRAD ? share + u * (0.39894228f * __expf(-0.5f * u * u)) : u * share;
+        const float a = fabsf(u), t = __builtin_amdgcn_rcpf(fmaf(0.33f, a, 1.f));
+        const float exponential = __builtin_amdgcn_exp2f(u * u * -0.72134752f);
+        float q = fmaf(-0.11074109f, t, 0.37948442f);
+        q = fmaf(q, t, -0.09645796f);
+        q = fmaf(q, t, 0.20633404f);
+        q = fmaf(q, t, 0.12138055f);
+        q *= t * exponential;
+        const float share = u < 0.f ? q : 1.f - q;
+        return GRAD ? fmaf(u * 0.39894228f, exponential, share) : u * share;
     } else {
-        const float u2 = fminf(u * u, 1e4f);                  // tanh is 1 long before; the square stays finite
-        const float t = tanhf(0.79788456f * u * (1.f + 0.044715f * u2));
-        const float share = 0.5f * (1.f + t);
-        return GRAD ? share + u * (0.5f * (1.f - t * t) * 0.79788456f * (1.f + 0.134145f * u2)) : u * share;
+        const float u2 = fminf(u * u, 1e4f);                  // the share is 0 or 1 long before; the square stays finite
+        const float share = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.3022082f * u * fmaf(0.044715f, u2, 1.f)));
+        return GRAD ? fmaf(u * (share * (1.f - share)) * 1.5957691f, fmaf(0.134145f, u2, 1.f), share) : u * share;
     }
 }
 
-template <int DT, int PDT, int FORM, bool GRAD>
+// Workgroups of 256 threads as 2^lanes_log2 lanes of a chunk each by the rest of the rows; a thread keeps its columns (and their
+// bias and, for gradients, their sums) and takes kGeluRows rows at a time.
+constexpr int kGeluRows = 4;
+
+template <int DT, int FORM, bool GRAD>
 __global__ void __launch_bounds__(kThreads) gelu_kernel(const GeluArgs p)
 {
-    for (uint32_t r = blockIdx.x; r < p.rows; r += gridDim.x)
-        for (uint32_t c = threadIdx.x; c < p.cols; c += kThreads) {
-            const float u = load_one<DT>(p.x, r * p.ld_x + c) + (p.bias ? load_one<PDT>(p.bias, c) : 0.f);
-            float v = gelu<FORM, GRAD>(u);
-            if constexpr (GRAD)
-                v *= load_one<DT>(p.dy, r * p.ld_dy + c);
-            store_one<DT>(p.out, r * p.ld_out + c, v);
+    constexpr int N = kElems<DT>;
+    const uint32_t lanes = 1u << p.lanes_log2, high = kThreads >> p.lanes_log2;
+    const uint32_t group = blockIdx.x % p.groups, strip = blockIdx.x / p.groups;
+    const uint32_t chunk = group * lanes + (threadIdx.x & (lanes - 1u)), y = threadIdx.x >> p.lanes_log2;
+    const uint32_t c = chunk * N, left = chunk >= p.chunks ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
+    float b[N], sum[N];
+#pragma unroll
+    for (int e = 0; e < N; e++)
+        b[e] = sum[e] = 0.f;
+    if (p.bias && left)
+        load_params<N>(p.bias, p.param_f32, c, left, b);
+    const uint32_t step = p.strips * high;
+    if (left)
+        for (uint64_t r0 = strip * high + y; r0 < p.rows; r0 += (uint64_t)kGeluRows * step) {
+            u32x4 x[kGeluRows], d[kGeluRows];
+#pragma unroll
+            for (int i = 0; i < kGeluRows; i++) {
+                const uint64_t r = r0 + (uint64_t)i * step;
+                x[i] = d[i] = u32x4{0u, 0u, 0u, 0u};
+                if (r < p.rows) {
+                    x[i] = load_chunk<DT>(p.x, r * p.ld_x + c, left);
+                    if constexpr (GRAD)
+                        d[i] = load_chunk<DT>(p.dy, r * p.ld_dy + c, left);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kGeluRows; i++) {
+                const uint64_t r = r0 + (uint64_t)i * step;
+                if (r < p.rows) {
+                    float v[N], u[N];
+                    unpack<DT>(x[i], v);
+                    unpack<DT>(d[i], u);
+#pragma unroll
+                    for (int e = 0; e < N; e++) {
+                        v[e] = gelu<FORM, GRAD>(v[e] + b[e]);
+                        if constexpr (GRAD) {
+                            v[e] *= u[e];
+                            sum[e] += (uint32_t)e < left ? v[e] : 0.f;
+                        }
+                    }
+                    store_chunk<DT>(p.out, r * p.ld_out + c, left, pack<DT>(v));
+                }
+            }
         }
+    if constexpr (GRAD) {
+        if (!p.dbias)
+            return;
+        __shared__ float sums[kThreads * N];                                    // [y][lane][element]
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            sums[threadIdx.x * N + e] = sum[e];
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < lanes * N; i += kThreads) {
+            const uint32_t col = group * lanes * N + i;
+            float s = 0.f;
+            for (uint32_t k = 0; k < high; k++)
+                s += sums[k * lanes * N + i];
+            if (col < p.cols) {
+                if (p.strips > 1)
+                    p.partial[(size_t)strip * p.pitch + col] = s;
+                else
+                    store_param(p.dbias, p.param_f32, col, s);
+            }
+        }
+    }
 }
 
-template <int DT, int PDT, int FORM>
-__global__ void __launch_bounds__(kThreads) gelu_columns_kernel(const GeluArgs p)
-{
-    const uint32_t c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= p.cols)
-        return;
-    const float b = p.bias ? load_one<PDT>(p.bias, c) : 0.f;
-    float s = 0.f;
-    for (uint32_t r = blockIdx.y; r < p.rows; r += p.strips)
-        s += load_one<DT>(p.dy, r * p.ld_dy + c) * gelu<FORM, true>(load_one<DT>(p.x, r * p.ld_x + c) + b);
-    p.partial[(size_t)blockIdx.y * p.cols + c] = s;
-}
-
-template <int PDT>
+// Adds up the strips' sums: 8 lanes take 32 neighbouring columns (a line of 128 bytes), 32 of these groups every 32nd strip.
 __global__ void __launch_bounds__(kThreads) columns_kernel(const ColumnArgs p)
 {
-    const uint32_t c = blockIdx.x * kThreads + threadIdx.x;
     void *const out = p.out[blockIdx.y];
-    if (c >= p.cols || !out)
+    if (!out)
         return;
-    float s = 0.f;
-    for (uint32_t k = 0; k < p.strips; k++)
-        s += p.partial[((size_t)k * p.sums + blockIdx.y) * p.cols + c];
-    store_one<PDT>(out, c, s);
+    __shared__ float sums[32][33];
+    const uint32_t x = threadIdx.x % 8u, y = threadIdx.x / 8u, c = blockIdx.x * 32u + x * 4u;
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (c < p.cols)                                                             // the pitch is a multiple of four
+#pragma unroll 4
+        for (uint32_t k = y; k < p.strips; k += 32u)
+            s += *(const f32x4 *)(p.partial + ((size_t)k * p.sums + blockIdx.y) * p.pitch + c);
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        sums[y][x * 4 + e] = s[e];
+    __syncthreads();
+    if (threadIdx.x < 32u && blockIdx.x * 32u + threadIdx.x < p.cols) {
+        float t = 0.f;
+#pragma unroll
+        for (int k = 0; k < 32; k++)
+            t += sums[k][threadIdx.x];
+        store_param(out, p.param_f32, blockIdx.x * 32u + threadIdx.x, t);
+    }
 }
 
-constexpr uint32_t kMaxStrips = 512;
+// ---------------------------------------------------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------------------------------------------------
+// How a row is held, by its width.
+struct NormShape {
+    uint32_t cols, rows, grad_rows;                                             // the widest row; rows of a workgroup at a time
+    uint32_t threads, grad_threads;
+    void (*kernel[2])(const NormArgs);
+    void (*grad[2])(const NormGradArgs);
+};
 
-static uint32_t strips_of(int64_t rows) { return (uint32_t)(rows < (int64_t)kMaxStrips ? rows : kMaxStrips); }
+#define NORM_SHAPE(LANES, E)                                                                                        \
+    {LANES * E, kNormThreads<LANES> / LANES, kNormGradThreads<LANES> / LANES, kNormThreads<LANES>, kNormGradThreads<LANES>, \
+     {norm_kernel<kF32, LANES, E>, norm_kernel<kBF16, LANES, E>}, {norm_grad_kernel<kF32, LANES, E>, norm_grad_kernel<kBF16, LANES, E>}}
+static const NormShape kNormShapes[] = {NORM_SHAPE(8, 8), NORM_SHAPE(16, 8), NORM_SHAPE(32, 8), NORM_SHAPE(64, 8), NORM_SHAPE(64, 16),
+                                        NORM_SHAPE(256, 8), NORM_SHAPE(256, 16), NORM_SHAPE(512, 16), NORM_SHAPE(1024, 16)};
+#undef NORM_SHAPE
+
+static const NormShape *norm_shape(int64_t cols)
+{
+    for (const NormShape &s : kNormShapes)
+        if (cols <= s.cols)
+            return &s;
+    return nullptr;
+}
+
+static uint32_t at_most(uint64_t v, uint32_t most) { return (uint32_t)(v < most ? v : most); }
+
+static uint32_t pitch_of(int64_t cols) { return (uint32_t)((cols + 3) & ~3ll); }
+
+static uint32_t norm_strips(int64_t rows, int64_t cols)
+{
+    const NormShape *const s = norm_shape(cols);
+    if (!s)
+        return at_most(rows, 64);
+    return at_most((rows + s->grad_rows - 1) / s->grad_rows, 131072 / s->grad_threads);
+}
+
+// The tile of GELU's kernels: as many lanes as waste least at the end of a row.
+static void gelu_tile(int64_t rows, int64_t cols, tmask_dtype dt, GeluArgs *p)
+{
+    const uint32_t n = dt == TMASK_F32 ? 4 : 8;
+    p->chunks = (uint32_t)((cols + n - 1) / n);
+    uint32_t best = 0, waste = ~0u;
+    for (uint32_t l = 8; l >= 3 && (l == 8 || p->chunks < 1u << 20); l--) {
+        const uint32_t lost = ((p->chunks + (1u << l) - 1) >> l << l) - p->chunks;
+        if (lost < waste) {
+            waste = lost;
+            best = l;
+        }
+    }
+    p->lanes_log2 = best;
+    p->groups = (p->chunks + (1u << best) - 1) >> best;
+    const uint64_t high = kThreads >> best;
+    const uint64_t strips = (rows + high - 1) / high, most = (2048 + p->groups - 1) / p->groups;
+    p->strips = (uint32_t)(strips < most ? strips : most);
+    p->pitch = pitch_of(cols);
+}
+
+// columns such that a launch over them stays below 2^32 threads
+static bool norm_sizes(int64_t rows, int64_t cols) { return valid_sizes(rows, cols) && cols <= 1ll << 28; }
 
 static int check_head(int64_t rows, int64_t cols, tmask_dtype dt, tmask_dtype param_dt)
 {
     if (!known(dt) || !known(param_dt))
         return fail(TMASK_ERR_DTYPE, "unknown dtype %d or parameter dtype %d", (int)dt, (int)param_dt);
-    if (!valid_sizes(rows, cols))
-        return fail(TMASK_ERR_SHAPE, "rows=%lld cols=%lld", (long long)rows, (long long)cols);
+    if (!norm_sizes(rows, cols))
+        return fail(TMASK_ERR_SHAPE, "rows=%lld (below 2^31) cols=%lld (up to 2^28)", (long long)rows, (long long)cols);
     return TMASK_OK;
 }
 
-static uint32_t row_grid(int64_t rows) { return (uint32_t)(rows < 65536 ? rows : 65536); }
-
-static void sum_columns(const ColumnArgs &c, tmask_dtype param_dt, hipStream_t stream)
+static void sum_columns(const float *partial, void *out0, void *out1, int64_t cols, uint32_t strips, uint32_t sums, tmask_dtype param_dt, hipStream_t stream)
 {
-    const dim3 grid((c.cols + kThreads - 1) / kThreads, c.sums);
-    hipLaunchKernelGGL(param_dt == TMASK_F32 ? columns_kernel<kF32> : columns_kernel<kBF16>, grid, dim3(kThreads), 0, stream, c);
+    const ColumnArgs c{partial, {out0, out1}, (uint32_t)cols, strips, sums, pitch_of(cols), param_dt == TMASK_F32};
+    hipLaunchKernelGGL(columns_kernel, dim3((uint32_t)((cols + 31) / 32), sums), dim3(kThreads), 0, stream, c);
 }
 
 }  // namespace tmask
@@ -234,16 +725,19 @@ extern "C" int tmask_layer_norm(const tmask_norm_desc *desc, tmask_dtype dt, tma
     TMASK_TRY(check_vector("mean", d.mean, 4, d.rstd != nullptr));
     TMASK_TRY(check_vector("rstd", d.rstd, 4, d.mean != nullptr));
     NormArgs p{d.x, d.residual, d.weight, d.bias, d.y, d.total, d.mean, d.rstd, (size_t)d.ld_x, (size_t)d.ld_residual,
-               (size_t)d.ld_y, (size_t)d.ld_total, (uint32_t)d.rows, (uint32_t)d.cols, eps};
-    static void (*const kernels[2][2])(const NormArgs) = {{norm_kernel<kF32, kF32>, norm_kernel<kF32, kBF16>},
-                                                          {norm_kernel<kBF16, kF32>, norm_kernel<kBF16, kBF16>}};
-    hipLaunchKernelGGL(kernels[dt][param_dt], dim3(row_grid(d.rows)), dim3(kThreads), 0, (hipStream_t)hip_stream, p);
+               (size_t)d.ld_y, (size_t)d.ld_total, (uint32_t)d.rows, (uint32_t)d.cols, param_dt == TMASK_F32, eps, (float)(1.0 / (double)d.cols)};
+    hipStream_t stream = (hipStream_t)hip_stream;
+    if (const NormShape *const shape = norm_shape(d.cols))
+        hipLaunchKernelGGL(shape->kernel[dt], dim3(at_most((d.rows + shape->rows - 1) / shape->rows, 524288 / shape->threads)), dim3(shape->threads), 0,
+                           stream, p);
+    else
+        hipLaunchKernelGGL(dt == TMASK_F32 ? norm_long_kernel<kF32> : norm_long_kernel<kBF16>, dim3(at_most(d.rows, 512)), dim3(kLongThreads), 0, stream, p);
     return launched("layer norm launch");
 }
 
 extern "C" size_t tmask_layer_norm_workspace_bytes(int64_t rows, int64_t cols)
 {
-    return valid_sizes(rows, cols) ? (size_t)strips_of(rows) * 2u * (size_t)cols * 4u : 0;
+    return norm_sizes(rows, cols) ? (size_t)norm_strips(rows, cols) * 2u * pitch_of(cols) * 4u : 0;
 }
 
 extern "C" int tmask_layer_norm_backward(const tmask_norm_grad_desc *desc, tmask_dtype dt, tmask_dtype param_dt, void *workspace,
@@ -260,8 +754,11 @@ extern "C" int tmask_layer_norm_backward(const tmask_norm_grad_desc *desc, tmask
     if (d.rows == 0 && !sums)
         return TMASK_OK;
     hipStream_t stream = (hipStream_t)hip_stream;
-    NormGradArgs p{d.dy, d.x, d.weight, d.dtotal, d.mean, d.rstd, d.dx, (float *)workspace, (size_t)d.ld_dy, (size_t)d.ld_x,
-                   (size_t)d.ld_dtotal, (size_t)d.ld_dx, (uint32_t)d.rows, (uint32_t)d.cols, strips_of(d.rows)};
+    const uint32_t strips = norm_strips(d.rows, d.cols);
+    NormGradArgs p{d.dy, d.x, d.weight, d.dtotal, d.mean, d.rstd, d.dx, d.dweight, d.dbias, (float *)workspace, (size_t)d.ld_dy, (size_t)d.ld_x,
+                   (size_t)d.ld_dtotal, (size_t)d.ld_dx, (uint32_t)d.rows, (uint32_t)d.cols, param_dt == TMASK_F32, strips, pitch_of(d.cols),
+                   (float)(1.0 / (double)d.cols)};
+    const NormShape *const shape = norm_shape(d.cols);
     if (d.rows > 0) {
         TMASK_TRY(check_rows("dy", d.dy, d.ld_dy, d.rows, d.cols, size, true));
         TMASK_TRY(check_rows("x", d.x, d.ld_x, d.rows, d.cols, size, true));
@@ -270,18 +767,20 @@ extern "C" int tmask_layer_norm_backward(const tmask_norm_grad_desc *desc, tmask
         TMASK_TRY(check_vector("mean", d.mean, 4, true));
         TMASK_TRY(check_vector("rstd", d.rstd, 4, true));
         TMASK_TRY(check_vector("weight", d.weight, psize, false));
-        if (sums) {
+        if (sums)
             TMASK_TRY(check_workspace(workspace, workspace_bytes, tmask_layer_norm_workspace_bytes(d.rows, d.cols)));
-            // first, since dx may lie over dy or x
-            hipLaunchKernelGGL(dt == TMASK_F32 ? norm_columns_kernel<kF32> : norm_columns_kernel<kBF16>,
-                               dim3((p.cols + kThreads - 1) / kThreads, p.strips), dim3(kThreads), 0, stream, p);
+        if (shape) {
+            hipLaunchKernelGGL(shape->grad[dt], dim3(strips), dim3(shape->grad_threads), 0, stream, p);
+        } else {
+            if (sums)
+                hipLaunchKernelGGL(dt == TMASK_F32 ? norm_long_columns_kernel<kF32> : norm_long_columns_kernel<kBF16>,
+                                   dim3((p.cols + kThreads - 1) / kThreads, strips), dim3(kThreads), 0, stream, p);
+            hipLaunchKernelGGL(dt == TMASK_F32 ? norm_long_grad_kernel<kF32> : norm_long_grad_kernel<kBF16>, dim3(at_most(d.rows, 512)),
+                               dim3(kLongThreads), 0, stream, p);
         }
-        static void (*const kernels[2][2])(const NormGradArgs) = {{norm_grad_kernel<kF32, kF32>, norm_grad_kernel<kF32, kBF16>},
-                                                                  {norm_grad_kernel<kBF16, kF32>, norm_grad_kernel<kBF16, kBF16>}};
-        hipLaunchKernelGGL(kernels[dt][param_dt], dim3(row_grid(d.rows)), dim3(kThreads), 0, stream, p);
     }
-    if (sums)
-        sum_columns(ColumnArgs{p.partial, {d.dweight, d.dbias}, p.cols, p.strips, 2}, param_dt, stream);
+    if (sums && (strips != 1 || !shape))
+        sum_columns(p.partial, d.dweight, d.dbias, d.cols, strips, 2, param_dt, stream);
     return launched("layer norm gradient launch");
 }
 
@@ -290,8 +789,7 @@ static int check_form(tmask_gelu_form form)
     return form == TMASK_GELU_ERF || form == TMASK_GELU_TANH ? TMASK_OK : fail(TMASK_ERR_DTYPE, "unknown form of GELU %d", (int)form);
 }
 
-#define GELU_KERNELS(DT, PDT, GRAD) {gelu_kernel<DT, PDT, TMASK_GELU_ERF, GRAD>, gelu_kernel<DT, PDT, TMASK_GELU_TANH, GRAD>}
-#define GELU_COLUMNS(DT, PDT) {gelu_columns_kernel<DT, PDT, TMASK_GELU_ERF>, gelu_columns_kernel<DT, PDT, TMASK_GELU_TANH>}
+#define GELU_KERNELS(DT, GRAD) {gelu_kernel<DT, TMASK_GELU_ERF, GRAD>, gelu_kernel<DT, TMASK_GELU_TANH, GRAD>}
 
 extern "C" int tmask_bias_gelu(const tmask_gelu_desc *desc, tmask_dtype dt, tmask_dtype param_dt, tmask_gelu_form form, void *hip_stream)
 {
@@ -305,16 +803,25 @@ extern "C" int tmask_bias_gelu(const tmask_gelu_desc *desc, tmask_dtype dt, tmas
     TMASK_TRY(check_rows("x", d.x, d.ld_x, d.rows, d.cols, size_of(dt), true));
     TMASK_TRY(check_rows("y", d.y, d.ld_y, d.rows, d.cols, size_of(dt), true));
     TMASK_TRY(check_vector("bias", d.bias, size_of(param_dt), false));
-    GeluArgs p{nullptr, d.x, d.bias, d.y, nullptr, 0, (size_t)d.ld_x, (size_t)d.ld_y, (uint32_t)d.rows, (uint32_t)d.cols, 0};
-    static void (*const kernels[2][2][2])(const GeluArgs) = {{GELU_KERNELS(kF32, kF32, false), GELU_KERNELS(kF32, kBF16, false)},
-                                                             {GELU_KERNELS(kBF16, kF32, false), GELU_KERNELS(kBF16, kBF16, false)}};
-    hipLaunchKernelGGL(kernels[dt][param_dt][form], dim3(row_grid(d.rows)), dim3(kThreads), 0, (hipStream_t)hip_stream, p);
+    GeluArgs p{nullptr, d.x, d.bias, d.y, nullptr, nullptr, 0, (size_t)d.ld_x, (size_t)d.ld_y, (uint32_t)d.rows, (uint32_t)d.cols, 0,
+               param_dt == TMASK_F32, 0, 0, 0, 0};
+    gelu_tile(d.rows, d.cols, dt, &p);
+    static void (*const kernels[2][2])(const GeluArgs) = {GELU_KERNELS(kF32, false), GELU_KERNELS(kBF16, false)};
+    hipLaunchKernelGGL(kernels[dt][form], dim3(p.groups * p.strips), dim3(kThreads), 0, (hipStream_t)hip_stream, p);
     return launched("GELU launch");
 }
 
 extern "C" size_t tmask_bias_gelu_workspace_bytes(int64_t rows, int64_t cols)
 {
-    return valid_sizes(rows, cols) ? (size_t)strips_of(rows) * (size_t)cols * 4u : 0;
+    if (!norm_sizes(rows, cols))
+        return 0;
+    size_t strips = 0;
+    for (const tmask_dtype dt : {TMASK_F32, TMASK_BF16}) {
+        GeluArgs p;
+        gelu_tile(rows, cols, dt, &p);
+        strips = p.strips > strips ? p.strips : strips;
+    }
+    return strips * pitch_of(cols) * 4u;
 }
 
 extern "C" int tmask_bias_gelu_backward(const tmask_gelu_grad_desc *desc, tmask_dtype dt, tmask_dtype param_dt, tmask_gelu_form form,
@@ -329,24 +836,20 @@ extern "C" int tmask_bias_gelu_backward(const tmask_gelu_grad_desc *desc, tmask_
     if (d.rows == 0 && !d.dbias)
         return TMASK_OK;
     hipStream_t stream = (hipStream_t)hip_stream;
-    GeluArgs p{d.dy, d.x, d.bias, d.dx, (float *)workspace, (size_t)d.ld_dy, (size_t)d.ld_x, (size_t)d.ld_dx, (uint32_t)d.rows,
-               (uint32_t)d.cols, strips_of(d.rows)};
+    GeluArgs p{d.dy, d.x, d.bias, d.dx, d.dbias, (float *)workspace, (size_t)d.ld_dy, (size_t)d.ld_x, (size_t)d.ld_dx, (uint32_t)d.rows,
+               (uint32_t)d.cols, 0, param_dt == TMASK_F32, 0, 0, 0, 0};
+    gelu_tile(d.rows, d.cols, dt, &p);
     if (d.rows > 0) {
         TMASK_TRY(check_rows("dy", d.dy, d.ld_dy, d.rows, d.cols, size_of(dt), true));
         TMASK_TRY(check_rows("x", d.x, d.ld_x, d.rows, d.cols, size_of(dt), true));
         TMASK_TRY(check_rows("dx", d.dx, d.ld_dx, d.rows, d.cols, size_of(dt), true));
         TMASK_TRY(check_vector("bias", d.bias, size_of(param_dt), false));
-        if (d.dbias) {
+        if (d.dbias)
             TMASK_TRY(check_workspace(workspace, workspace_bytes, tmask_bias_gelu_workspace_bytes(d.rows, d.cols)));
-            static void (*const columns[2][2][2])(const GeluArgs) = {{GELU_COLUMNS(kF32, kF32), GELU_COLUMNS(kF32, kBF16)},
-                                                                     {GELU_COLUMNS(kBF16, kF32), GELU_COLUMNS(kBF16, kBF16)}};
-            hipLaunchKernelGGL(columns[dt][param_dt][form], dim3((p.cols + kThreads - 1) / kThreads, p.strips), dim3(kThreads), 0, stream, p);
-        }
-        static void (*const kernels[2][2][2])(const GeluArgs) = {{GELU_KERNELS(kF32, kF32, true), GELU_KERNELS(kF32, kBF16, true)},
-                                                                 {GELU_KERNELS(kBF16, kF32, true), GELU_KERNELS(kBF16, kBF16, true)}};
-        hipLaunchKernelGGL(kernels[dt][param_dt][form], dim3(row_grid(d.rows)), dim3(kThreads), 0, stream, p);
+        static void (*const kernels[2][2])(const GeluArgs) = {GELU_KERNELS(kF32, true), GELU_KERNELS(kBF16, true)};
+        hipLaunchKernelGGL(kernels[dt][form], dim3(p.groups * p.strips), dim3(kThreads), 0, stream, p);
     }
-    if (d.dbias)
-        sum_columns(ColumnArgs{p.partial, {d.dbias, nullptr}, p.cols, p.strips, 1}, param_dt, stream);
+    if (d.dbias && p.strips != 1)
+        sum_columns(p.partial, d.dbias, nullptr, d.cols, p.strips, 1, param_dt, stream);
     return launched("GELU gradient launch");
 }

@@ -472,8 +472,8 @@ def test_rows_past_32_bits():
     tm.tmask_bias_gelu(x, y)
     tm.tmask_bias_gelu(near, out)
     same()
-    tm.tmask_bias_gelu_backward(x, x, y, dbias=sums[0], workspace=ws)
-    tm.tmask_bias_gelu_backward(near, near, out, dbias=sums[1], workspace=ws)
+    tm.tmask_bias_gelu_backward(x, x, y, dbias=sums[0], workspace=tm.alloc_bias_gelu_workspace(x))
+    tm.tmask_bias_gelu_backward(near, near, out, dbias=sums[1], workspace=tm.alloc_bias_gelu_workspace(x))
     same()
     assert torch.equal(sums[0], sums[1])
     teacher, index = lists(m, 4, 1000, 9, bf, 32)
