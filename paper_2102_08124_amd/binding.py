@@ -120,6 +120,7 @@ _calls = None
 class _ThroughCtypes:
     """In the place of _calls: every call is one for the code here."""
     batch = dense = score = spmm24 = staticmethod(lambda *args: None)
+    layer_norm = layer_norm_backward = bias_gelu = bias_gelu_backward = distill = distill_backward = staticmethod(lambda *args: None)
 
 
 def _native_calls():
@@ -200,7 +201,8 @@ def load_library():
     # addresses for the native calls
     L.at = {name: C.cast(getattr(L, name), vp).value for name in
             ("tmask_approx", "tmask_exact", "tmask_prune_1d", "tmask_apply_pack", "tmask_approx_pack", "tmask_approx_dense",
-             "tmask_score", "tmask_spmm24")}
+             "tmask_score", "tmask_spmm24", "tmask_layer_norm", "tmask_layer_norm_backward", "tmask_bias_gelu", "tmask_bias_gelu_backward",
+             "tmask_distill", "tmask_distill_backward")}
     _calls = _native_calls()
     _lib = L
     return L
@@ -534,6 +536,9 @@ def tmask_layer_norm(x: torch.Tensor, y: torch.Tensor, weight: Optional[torch.Te
     (fp32, one a row) the statistics that tmask_layer_norm_backward needs.  x, y, residual, total share a dtype, weight and bias
     another."""
     L = _lib or load_library()
+    rc = _calls.layer_norm(L.at["tmask_layer_norm"], x, y, weight, bias, residual, total, mean, rstd, eps, stream)
+    if rc is not None:
+        return None if rc == TMASK_OK else _check(rc)
     dt = _dtype_code_of(x.dtype, "x")
     px, rows, cols, ld = _mat2d(x, "x")
     pd = _param_dtype(weight, bias)
@@ -552,6 +557,9 @@ def tmask_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Ten
     statistics.  dx (plus dtotal, what reaches the residual stream by its other way) is the gradient of x and residual
     alike; dweight and dbias need a workspace (alloc_layer_norm_workspace)."""
     L = _lib or load_library()
+    rc = _calls.layer_norm_backward(L.at["tmask_layer_norm_backward"], dy, x, mean, rstd, dx, weight, dweight, dbias, dtotal, workspace, stream)
+    if rc is not None:
+        return None if rc == TMASK_OK else _check(rc)
     dt = _dtype_code_of(x.dtype, "x")
     px, rows, cols, ld = _mat2d(x, "x")
     pd = _param_dtype(weight, dweight, dbias)
@@ -566,6 +574,9 @@ def tmask_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Ten
 def tmask_bias_gelu(x: torch.Tensor, y: torch.Tensor, bias: Optional[torch.Tensor] = None, tanh: bool = False, stream=None) -> None:
     """y = GELU(x + bias), with erf or (tanh=True) in its form with tanh."""
     L = _lib or load_library()
+    rc = _calls.bias_gelu(L.at["tmask_bias_gelu"], x, y, bias, tanh, stream)
+    if rc is not None:
+        return None if rc == TMASK_OK else _check(rc)
     dt = _dtype_code_of(x.dtype, "x")
     px, rows, cols, ld = _mat2d(x, "x")
     pd = _param_dtype(bias)
@@ -578,6 +589,9 @@ def tmask_bias_gelu_backward(dy: torch.Tensor, x: torch.Tensor, dx: torch.Tensor
                              stream=None) -> None:
     """Gradients of tmask_bias_gelu from the same x and bias; dbias needs a workspace (alloc_bias_gelu_workspace)."""
     L = _lib or load_library()
+    rc = _calls.bias_gelu_backward(L.at["tmask_bias_gelu_backward"], dy, x, dx, bias, dbias, tanh, workspace, stream)
+    if rc is not None:
+        return None if rc == TMASK_OK else _check(rc)
     dt = _dtype_code_of(x.dtype, "x")
     px, rows, cols, ld = _mat2d(x, "x")
     pd = _param_dtype(bias, dbias)
@@ -608,6 +622,9 @@ def tmask_distill(logits: torch.Tensor, teacher: torch.Tensor, index: torch.Tens
     sum(row_weight * loss) in the same call; row_max and row_sum are what tmask_distill_backward needs later.
     workspace: alloc_distill_workspace."""
     L = _lib or load_library()
+    rc = _calls.distill(L.at["tmask_distill"], logits, teacher, index, temperature, loss, row_max, row_sum, dlogits, row_weight, workspace, stream)
+    if rc is not None:
+        return None if rc == TMASK_OK else _check(rc)
     d, dt, tdt, bits = _distill_desc(logits, teacher, index, loss, row_max, row_sum, dlogits, row_weight)
     wp, wb = _ws_args(workspace)
     _check(L.tmask_distill(d, dt, tdt, bits, temperature, wp, wb, _stream_ptr(stream)))
@@ -617,6 +634,9 @@ def tmask_distill_backward(logits: torch.Tensor, teacher: torch.Tensor, index: t
                            row_sum: torch.Tensor, dlogits: torch.Tensor, row_weight: Optional[torch.Tensor] = None, stream=None) -> None:
     """dlogits = the gradient of sum(row_weight * loss) of an earlier tmask_distill, from its row_max and row_sum."""
     L = _lib or load_library()
+    rc = _calls.distill_backward(L.at["tmask_distill_backward"], logits, teacher, index, temperature, row_max, row_sum, dlogits, row_weight, stream)
+    if rc is not None:
+        return None if rc == TMASK_OK else _check(rc)
     d, dt, tdt, bits = _distill_desc(logits, teacher, index, None, row_max, row_sum, dlogits, row_weight)
     _check(L.tmask_distill_backward(d, dt, tdt, bits, temperature, _stream_ptr(stream)))
 

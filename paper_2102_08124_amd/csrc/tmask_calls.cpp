@@ -228,7 +228,248 @@ PyObject *spmm24(PyObject *, PyObject *const *a, Py_ssize_t n)
         });
 }
 
-PyMethodDef kMethods[] = {{"batch", (PyCFunction)(void (*)(void))batch, METH_FASTCALL, nullptr},
+// The calls on rows: function, then the arguments of binding.py's function of that name in its order.  A tensor is 2-D with unit
+// column stride, a vector 1-D and contiguous; None is no tensor.
+bool as_float(PyObject *o, float *out)
+{
+    if (!PyFloat_CheckExact(o))
+        return false;
+    *out = (float)PyFloat_AS_DOUBLE(o);
+    return true;
+}
+
+bool as_bool(PyObject *o, bool *out)
+{
+    *out = o == Py_True;
+    return PyBool_Check(o);
+}
+
+struct Rows {
+    at::ScalarType type;
+    int64_t rows, cols;
+
+    // the tensor that the others have to fit
+    bool first(PyObject *o, const void **p, int64_t *ld)
+    {
+        const at::Tensor *t;
+        if (!as_tensor(o, &t) || t->dim() != 2 || !t->is_cuda())
+            return false;
+        type = t->scalar_type();
+        rows = t->size(0);
+        cols = t->size(1);
+        return (type == at::kFloat || type == at::kBFloat16) && fits(t, p, ld);
+    }
+    bool fits(const at::Tensor *t, const void **p, int64_t *ld) const
+    {
+        if (t->size(1) > 1 && t->stride(1) != 1)
+            return false;
+        *p = t->data_ptr();
+        *ld = t->stride(0);
+        return true;
+    }
+    bool other(PyObject *o, const void **p, int64_t *ld) const
+    {
+        *p = nullptr;
+        *ld = 0;
+        if (o == Py_None)
+            return true;
+        const at::Tensor *t;
+        return as_tensor(o, &t) && t->dim() == 2 && t->is_cuda() && t->scalar_type() == type && t->size(0) == rows && t->size(1) == cols && fits(t, p, ld);
+    }
+    bool other(PyObject *o, void **p, int64_t *ld) const { return other(o, (const void **)p, ld); }
+    tmask_dtype dtype() const { return type == at::kFloat ? TMASK_F32 : TMASK_BF16; }
+};
+
+bool as_vector(PyObject *o, at::ScalarType type, int64_t n, const void **p)
+{
+    *p = nullptr;
+    if (o == Py_None)
+        return true;
+    const at::Tensor *t;
+    if (!as_tensor(o, &t) || t->dim() != 1 || !t->is_cuda() || t->scalar_type() != type || t->size(0) != n || !t->is_contiguous())
+        return false;
+    *p = t->data_ptr();
+    return true;
+}
+
+template <typename T>
+bool as_floats(PyObject *o, int64_t n, T **p)
+{
+    return as_vector(o, at::kFloat, n, (const void **)p);
+}
+
+// weights, biases and their gradients: one type among them, fp32 if there are none
+struct Params {
+    at::ScalarType type = at::kFloat;
+    bool seen = false;
+
+    bool one(PyObject *o, int64_t n, const void **p)
+    {
+        const at::Tensor *t;
+        if (o != Py_None && !seen) {
+            if (!as_tensor(o, &t))
+                return false;
+            type = t->scalar_type();
+            seen = true;
+        }
+        return (type == at::kFloat || type == at::kBFloat16) && as_vector(o, type, n, p);
+    }
+    bool one(PyObject *o, int64_t n, void **p) { return one(o, n, (const void **)p); }
+    tmask_dtype dtype() const { return type == at::kFloat ? TMASK_F32 : TMASK_BF16; }
+};
+
+// layer_norm(function, x, y, weight, bias, residual, total, mean, rstd, eps, stream)
+PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 11)
+        Py_RETURN_NONE;
+    void *fn, *stream;
+    tmask_norm_desc d;
+    Rows x;
+    Params w;
+    float eps;
+    return run(
+        [&] {
+            if (!as_address(a[0], &fn) || !x.first(a[1], &d.x, &d.ld_x))
+                return false;
+            d.rows = x.rows;
+            d.cols = x.cols;
+            return x.other(a[2], &d.y, &d.ld_y) && w.one(a[3], x.cols, &d.weight) && w.one(a[4], x.cols, &d.bias) &&
+                   x.other(a[5], &d.residual, &d.ld_residual) && x.other(a[6], &d.total, &d.ld_total) && as_floats(a[7], x.rows, &d.mean) &&
+                   as_floats(a[8], x.rows, &d.rstd) && as_float(a[9], &eps) && as_stream(a[10], &stream);
+        },
+        [&] { return ((decltype(&tmask_layer_norm))fn)(&d, x.dtype(), w.dtype(), eps, stream); });
+}
+
+// layer_norm_backward(function, dy, x, mean, rstd, dx, weight, dweight, dbias, dtotal, workspace, stream)
+PyObject *layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 12)
+        Py_RETURN_NONE;
+    void *fn, *stream, *ws;
+    size_t bytes;
+    tmask_norm_grad_desc d;
+    Rows x;
+    Params w;
+    return run(
+        [&] {
+            if (!as_address(a[0], &fn) || !x.first(a[2], &d.x, &d.ld_x))
+                return false;
+            d.rows = x.rows;
+            d.cols = x.cols;
+            return x.other(a[1], &d.dy, &d.ld_dy) && as_floats(a[3], x.rows, &d.mean) && as_floats(a[4], x.rows, &d.rstd) &&
+                   x.other(a[5], &d.dx, &d.ld_dx) && w.one(a[6], x.cols, &d.weight) && w.one(a[7], x.cols, &d.dweight) && w.one(a[8], x.cols, &d.dbias) &&
+                   x.other(a[9], &d.dtotal, &d.ld_dtotal) && as_workspace(a[10], &ws, &bytes) && as_stream(a[11], &stream);
+        },
+        [&] { return ((decltype(&tmask_layer_norm_backward))fn)(&d, x.dtype(), w.dtype(), ws, bytes, stream); });
+}
+
+// bias_gelu(function, x, y, bias, tanh, stream)
+PyObject *bias_gelu(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 6)
+        Py_RETURN_NONE;
+    void *fn, *stream;
+    tmask_gelu_desc d;
+    Rows x;
+    Params b;
+    bool tanh;
+    return run(
+        [&] {
+            if (!as_address(a[0], &fn) || !x.first(a[1], &d.x, &d.ld_x))
+                return false;
+            d.rows = x.rows;
+            d.cols = x.cols;
+            return x.other(a[2], &d.y, &d.ld_y) && b.one(a[3], x.cols, &d.bias) && as_bool(a[4], &tanh) && as_stream(a[5], &stream);
+        },
+        [&] { return ((decltype(&tmask_bias_gelu))fn)(&d, x.dtype(), b.dtype(), tanh ? TMASK_GELU_TANH : TMASK_GELU_ERF, stream); });
+}
+
+// bias_gelu_backward(function, dy, x, dx, bias, dbias, tanh, workspace, stream)
+PyObject *bias_gelu_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 9)
+        Py_RETURN_NONE;
+    void *fn, *stream, *ws;
+    size_t bytes;
+    tmask_gelu_grad_desc d;
+    Rows x;
+    Params b;
+    bool tanh;
+    return run(
+        [&] {
+            if (!as_address(a[0], &fn) || !x.first(a[2], &d.x, &d.ld_x))
+                return false;
+            d.rows = x.rows;
+            d.cols = x.cols;
+            return x.other(a[1], &d.dy, &d.ld_dy) && x.other(a[3], &d.dx, &d.ld_dx) && b.one(a[4], x.cols, &d.bias) && b.one(a[5], x.cols, &d.dbias) &&
+                   as_bool(a[6], &tanh) && as_workspace(a[7], &ws, &bytes) && as_stream(a[8], &stream);
+        },
+        [&] {
+            return ((decltype(&tmask_bias_gelu_backward))fn)(&d, x.dtype(), b.dtype(), tanh ? TMASK_GELU_TANH : TMASK_GELU_ERF, ws, bytes, stream);
+        });
+}
+
+// what both calls of the distillation have: logits, teacher, index, temperature, row_max, row_sum, dlogits, row_weight
+bool as_distill(PyObject *logits, PyObject *teacher, PyObject *index, PyObject *row_max, PyObject *row_sum, PyObject *dlogits, PyObject *row_weight,
+                tmask_distill_desc *d, Rows *z, Rows *t, int *bits)
+{
+    const at::Tensor *i;
+    if (!z->first(logits, &d->logits, &d->ld_logits) || !t->first(teacher, &d->teacher, &d->ld_teacher) || t->rows != z->rows || !as_tensor(index, &i))
+        return false;
+    if (i->scalar_type() != at::kInt && i->scalar_type() != at::kLong)
+        return false;
+    *bits = i->scalar_type() == at::kInt ? 32 : 64;
+    Rows whole = *t;
+    whole.type = i->scalar_type();
+    d->rows = z->rows;
+    d->vocab = z->cols;
+    d->k = t->cols;
+    return whole.other(index, &d->index, &d->ld_index) && as_floats(row_max, z->rows, &d->row_max) && as_floats(row_sum, z->rows, &d->row_sum) &&
+           z->other(dlogits, &d->dlogits, &d->ld_dlogits) && as_floats(row_weight, z->rows, &d->row_weight);
+}
+
+// distill(function, logits, teacher, index, temperature, loss, row_max, row_sum, dlogits, row_weight, workspace, stream)
+PyObject *distill(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 12)
+        Py_RETURN_NONE;
+    void *fn, *stream, *ws;
+    size_t bytes;
+    tmask_distill_desc d;
+    Rows z, t;
+    int bits;
+    float temperature;
+    return run(
+        [&] {
+            return as_address(a[0], &fn) && as_distill(a[1], a[2], a[3], a[6], a[7], a[8], a[9], &d, &z, &t, &bits) && as_float(a[4], &temperature) &&
+                   as_floats(a[5], z.rows, &d.loss) && as_workspace(a[10], &ws, &bytes) && as_stream(a[11], &stream);
+        },
+        [&] { return ((decltype(&tmask_distill))fn)(&d, z.dtype(), t.dtype(), bits, temperature, ws, bytes, stream); });
+}
+
+// distill_backward(function, logits, teacher, index, temperature, row_max, row_sum, dlogits, row_weight, stream)
+PyObject *distill_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 10)
+        Py_RETURN_NONE;
+    void *fn, *stream;
+    tmask_distill_desc d;
+    Rows z, t;
+    int bits;
+    float temperature;
+    return run(
+        [&] {
+            d.loss = nullptr;
+            return as_address(a[0], &fn) && as_distill(a[1], a[2], a[3], a[5], a[6], a[7], a[8], &d, &z, &t, &bits) && as_float(a[4], &temperature) &&
+                   as_stream(a[9], &stream);
+        },
+        [&] { return ((decltype(&tmask_distill_backward))fn)(&d, z.dtype(), t.dtype(), bits, temperature, stream); });
+}
+
+#define METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
+PyMethodDef kMethods[] = {METHOD(layer_norm), METHOD(layer_norm_backward), METHOD(bias_gelu), METHOD(bias_gelu_backward), METHOD(distill), METHOD(distill_backward),
+                          {"batch", (PyCFunction)(void (*)(void))batch, METH_FASTCALL, nullptr},
                           {"dense", (PyCFunction)(void (*)(void))dense, METH_FASTCALL, nullptr},
                           {"score", (PyCFunction)(void (*)(void))score, METH_FASTCALL, nullptr},
                           {"spmm24", (PyCFunction)(void (*)(void))spmm24, METH_FASTCALL, nullptr},

@@ -103,9 +103,69 @@ __device__ __forceinline__ float share_of(const DistillArgs &a, const List &l, i
     return s;
 }
 
+// Running maximum and sum of exponentials of one lane: sum is relative to the maximum, or to 0 where that is -Inf (then it is 0, or
+// NaN if there was one).
+struct Running {
+    float max, sum;
+};
+
+// G chunks more, at a price of one exponential for the sum so far.  The empty statement keeps the compiler from holding
+// the unpacked elements of a row, twice its registers, until the gradient.
+template <int DT, int G>
+__device__ __forceinline__ void add_chunks(const DistillArgs &a, Running &run, u32x4 (&raw)[G])
+{
+    constexpr int N = kElems<DT>;
+    float v[N], m = run.max, s = 0.f;
+#pragma unroll
+    for (int i = 0; i < G; i++) {
+        unpack<DT>(raw[i], v);
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            m = fmaxf(m, v[e]);
+        asm volatile("" : "+v"(raw[i]));
+    }
+    const float to = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < G; i++) {
+        unpack<DT>(raw[i], v);
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            s += exp_of(a, v[e] - to);
+        asm volatile("" : "+v"(raw[i]));
+    }
+    run.sum = run.sum * (run.max == -INFINITY ? 1.f : exp_of(a, run.max - to)) + s;
+    run.max = m;
+}
+
+// What `run` counts relative to the maximum of all; all -Inf: NaN, as the formula has it.
+__device__ __forceinline__ float relative(const DistillArgs &a, Running run, float max)
+{
+    return run.max == -INFINITY && max != -INFINITY ? run.sum : run.sum * exp_of(a, run.max - max);
+}
+
+template <int DT>
+__device__ __forceinline__ u32x4 no_chunk()
+{
+    constexpr uint32_t kNone = DT == kF32 ? 0xFF800000u : 0xFF80FF80u;          // -Inf
+    return u32x4{kNone, kNone, kNone, kNone};
+}
+
+// the gradient of a chunk without the teacher's part
+template <int DT>
+__device__ __forceinline__ u32x4 pull(const DistillArgs &a, u32x4 raw, float z_max, float g_q)
+{
+    constexpr int N = kElems<DT>;
+    float v[N];
+    unpack<DT>(raw, v);
+#pragma unroll
+    for (int e = 0; e < N; e++)
+        v[e] = exp_of(a, v[e] - z_max) * g_q;
+    return pack<DT>(v);
+}
+
 // ---------------------------------------------------------------------------------------------------------------------
-// A row in the registers of one workgroup: T threads with P chunks each.  The logits are read once; the maximum, the sum and
-// the gradient are taken from registers.  (The chunk that a row ends inside, if its length is odd, is thread 0's.)
+// A row in the registers of one workgroup: T threads with P chunks each.  The logits are read once, added up as they arrive, and the
+// gradient is taken from the registers.  (The chunk that a row ends inside, if its length is odd, is thread 0's.)
 //
 // The gradient's columns that the list names are written again, with what the teacher takes from them, when the rest has been
 // written: k of the vocabulary's columns, and the barrier between orders the two.
@@ -113,25 +173,24 @@ __device__ __forceinline__ float share_of(const DistillArgs &a, const List &l, i
 template <int DT, int T, int P>
 __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
 {
-    constexpr int N = kElems<DT>, W = T / 64;
-    constexpr uint32_t kNone = DT == kF32 ? 0xFF800000u : 0xFF80FF80u;          // -Inf
+    constexpr int N = kElems<DT>, W = T / 64, G = 4;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     float *const red = (float *)lds;                                            // 2 x 2 W numbers, and W
     const List list = list_in(red + 5 * W, a);
     for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const size_t z0 = r * a.ld_logits;
-        u32x4 raw[P], last = u32x4{kNone, kNone, kNone, kNone};
+        u32x4 raw[P / G][G], last[1] = {no_chunk<DT>()};
         const bool has_last = a.tail && threadIdx.x == 0;
 #pragma unroll
         for (int i = 0; i < P; i++) {
             const uint32_t c = threadIdx.x + (uint32_t)(i * T);
-            raw[i] = u32x4{kNone, kNone, kNone, kNone};
+            raw[i / G][i % G] = no_chunk<DT>();
             if (c < a.full)
-                raw[i] = load_chunk<DT>(a.logits, z0 + (size_t)c * N, N);
+                raw[i / G][i % G] = load_whole<DT>((const unsigned char *)a.logits + z0 * kSize<DT> + (size_t)(i * T) * 16u, threadIdx.x * 16u);
         }
         if (has_last)
-            last = load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail, -INFINITY);
-        float t_max = -INFINITY, z_max = -INFINITY;
+            last[0] = load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail, -INFINITY);
+        float t_max = -INFINITY;
         if (a.k) {
             clear_table<T>(a, list);
             __syncthreads();
@@ -145,35 +204,16 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
                 }
             }
         }
-        float v[N];
+        Running run = {-INFINITY, 0.f};
 #pragma unroll
-        for (int i = 0; i < P; i++) {
-            unpack<DT>(raw[i], v);
-#pragma unroll
-            for (int e = 0; e < N; e++)
-                z_max = fmaxf(z_max, v[e]);
-        }
-        unpack<DT>(last, v);
-#pragma unroll
-        for (int e = 0; e < N; e++)
-            z_max = fmaxf(z_max, v[e]);
+        for (int i = 0; i < P / G; i++)
+            if ((uint32_t)(i * G * T) < a.full)
+                add_chunks<DT, G>(a, run, raw[i]);
+        if (has_last)
+            add_chunks<DT, 1>(a, run, last);
+        float z_max = run.max;
         group_reduce<Max, Max, W>(t_max, z_max, red);
-
-        float t_sum = 0.f, z_sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < P; i++)
-            if ((uint32_t)(i * T) < a.full) {
-                unpack<DT>(raw[i], v);
-#pragma unroll
-                for (int e = 0; e < N; e++)
-                    z_sum += exp_of(a, v[e] - z_max);
-            }
-        if (has_last) {
-            unpack<DT>(last, v);
-#pragma unroll
-            for (int e = 0; e < N; e++)
-                z_sum += exp_of(a, v[e] - z_max);
-        }
+        float t_sum = 0.f, z_sum = relative(a, run, z_max);
         for (uint32_t j = threadIdx.x; j < a.k; j += T)
             if (list.at[j] >= 0)
                 t_sum += exp_of(a, list.t[j] - t_max);
@@ -201,21 +241,12 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
 #pragma unroll
             for (int i = 0; i < P; i++) {
                 const uint32_t c = threadIdx.x + (uint32_t)(i * T);
-                if (c < a.full) {
-                    unpack<DT>(raw[i], v);
-#pragma unroll
-                    for (int e = 0; e < N; e++)
-                        v[e] = none ? 0.f : exp_of(a, v[e] - z_max) * g_q;
-                    store_chunk<DT>(a.dlogits, d0 + (size_t)c * N, N, pack<DT>(v));
-                }
+                if (c < a.full)
+                    store_whole<DT>((unsigned char *)a.dlogits + d0 * kSize<DT> + (size_t)(i * T) * 16u, threadIdx.x * 16u,
+                                    none ? u32x4{0u, 0u, 0u, 0u} : pull<DT>(a, raw[i / G][i % G], z_max, g_q));
             }
-            if (has_last) {
-                unpack<DT>(last, v);
-#pragma unroll
-                for (int e = 0; e < N; e++)
-                    v[e] = none ? 0.f : exp_of(a, v[e] - z_max) * g_q;
-                store_chunk<DT>(a.dlogits, d0 + (size_t)a.full * N, a.tail, pack<DT>(v));
-            }
+            if (has_last)
+                store_chunk<DT>(a.dlogits, d0 + (size_t)a.full * N, a.tail, none ? u32x4{0u, 0u, 0u, 0u} : pull<DT>(a, last[0], z_max, g_q));
         }
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -243,10 +274,12 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Few rows, or rows that no workgroup holds: parts of rows.  The first launch takes the maximum and the sum of each part
-// (relative to its own maximum, or to 0 where that is -Inf, so that a part that is masked has sum 0) and the student's logits of the
-// entries in it; the second joins them and does the rest, part by part, from logits that the caches may still hold.
+// Few rows, or rows that no workgroup holds: parts of rows.  The first launch takes the maximum and the sum of each part and the
+// student's logits of the entries in it; the second joins them and does the rest, part by part, from logits that the caches may
+// still hold.
 // ---------------------------------------------------------------------------------------------------------------------
+constexpr int kAhead = 8;                 // chunks that a thread has in flight
+
 struct Part {
     uint32_t r, part, begin, end;         // row, part, chunks
     bool last;                            // the row's last part: the elements behind the chunks are its own
@@ -271,56 +304,42 @@ __device__ __forceinline__ bool in_part(const DistillArgs &a, const Part &p, int
 }
 
 template <int DT>
+__device__ __forceinline__ void fetch(const DistillArgs &a, const Part &p, uint32_t c0, u32x4 (&raw)[kAhead])
+{
+#pragma unroll
+    for (int i = 0; i < kAhead; i++) {
+        const uint32_t c = c0 + threadIdx.x + (uint32_t)i * kSlice;
+        raw[i] = no_chunk<DT>();
+        if (c < p.end)
+            raw[i] = load_whole<DT>((const unsigned char *)a.logits + p.r * a.ld_logits * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u);
+    }
+}
+
+template <int DT>
 __global__ void __launch_bounds__(kSlice) distill_part_kernel(const DistillArgs a)
 {
-    constexpr int N = kElems<DT>, W = kSlice / 64, P = 4;
-    constexpr uint32_t kNone = DT == kF32 ? 0xFF800000u : 0xFF80FF80u;
+    constexpr int N = kElems<DT>, W = kSlice / 64;
     __shared__ float red[4 * W];
     for (uint64_t id = blockIdx.x; id < (uint64_t)a.rows * a.parts; id += gridDim.x) {
         const Part p = part_of(a, id);
         const size_t z0 = p.r * a.ld_logits;
-        float z_max = -INFINITY, z_sum = 0.f, v[N];
-        for (uint32_t c0 = p.begin; c0 < p.end || (c0 == p.begin && p.last); c0 += P * kSlice) {
-            u32x4 raw[P + 1];
-            float m = z_max;
-#pragma unroll
-            for (int i = 0; i <= P; i++)
-                raw[i] = u32x4{kNone, kNone, kNone, kNone};
-#pragma unroll
-            for (int i = 0; i < P; i++) {
-                const uint32_t c = c0 + threadIdx.x + (uint32_t)i * kSlice;
-                if (c < p.end)
-                    raw[i] = load_chunk<DT>(a.logits, z0 + (size_t)c * N, N);
-            }
-            const bool tail = a.tail && p.last && c0 == p.begin && threadIdx.x == 0;
-            if (tail)
-                raw[P] = load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail, -INFINITY);
-#pragma unroll
-            for (int i = 0; i <= P; i++) {
-                unpack<DT>(raw[i], v);
-#pragma unroll
-                for (int e = 0; e < N; e++)
-                    m = fmaxf(m, v[e]);
-            }
-            const float to = m == -INFINITY ? 0.f : m;
-            z_sum *= z_max == -INFINITY ? 1.f : exp_of(a, z_max - to);           // from 0 to a maximum: the sum is 0 or NaN
-            z_max = m;
-#pragma unroll
-            for (int i = 0; i <= P; i++)
-                if (i < P || tail) {
-                    unpack<DT>(raw[i], v);
-#pragma unroll
-                    for (int e = 0; e < N; e++)
-                        z_sum += exp_of(a, v[e] - to);
-                }
+        Running run = {-INFINITY, 0.f};
+        for (uint32_t c0 = p.begin; c0 < p.end; c0 += kAhead * kSlice) {
+            u32x4 raw[kAhead];
+            fetch<DT>(a, p, c0, raw);
+            add_chunks<DT, kAhead>(a, run, raw);
         }
-        float all = z_max, unused = 0.f;
+        if (a.tail && p.last && threadIdx.x == 0) {
+            u32x4 last[1] = {load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail, -INFINITY)};
+            add_chunks<DT, 1>(a, run, last);
+        }
+        float all = run.max, unused = 0.f;
         group_reduce<Max, Max, W>(all, unused, red);
-        z_sum *= z_max == -INFINITY ? 1.f : exp_of(a, z_max - all);
-        group_reduce<Sum, Sum, W>(z_sum, unused, red + 2 * W);
+        float sum = run.max == -INFINITY ? run.sum : relative(a, run, all);
+        group_reduce<Sum, Sum, W>(sum, unused, red + 2 * W);
         if (threadIdx.x == 0) {
             a.part_stats[2 * id] = all;
-            a.part_stats[2 * id + 1] = z_sum;
+            a.part_stats[2 * id + 1] = sum;
         }
         for (uint32_t j = threadIdx.x; j < a.k; j += kSlice) {
             const size_t i = p.r * a.ld_index + j;
@@ -337,7 +356,7 @@ __global__ void __launch_bounds__(kSlice) distill_part_kernel(const DistillArgs 
 template <int DT, bool JOIN>
 __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs a)
 {
-    constexpr int N = kElems<DT>, W = kSlice / 64, P = 4;
+    constexpr int N = kElems<DT>, W = kSlice / 64;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     float *const red = (float *)lds;
     const List list = list_in(red + 5 * W, a);
@@ -346,6 +365,9 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
         if (JOIN && !a.dlogits && p.part)                                       // the loss alone is joined by one workgroup a row
             continue;
         const size_t z0 = p.r * a.ld_logits;
+        u32x4 raw[kAhead];
+        if (a.dlogits)
+            fetch<DT>(a, p, p.begin, raw);
         float z_max, z_sum;
         if constexpr (JOIN) {
             const uint32_t lane = threadIdx.x & 63;
@@ -355,8 +377,7 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
                 s = a.part_stats[2 * ((uint64_t)p.r * a.parts + lane) + 1];
             }
             z_max = lanes_reduce<Max, 64>(m);
-            // all parts masked: NaN, as for a row in registers
-            z_sum = lanes_reduce<Sum, 64>(lane >= a.parts ? 0.f : m == -INFINITY && z_max != -INFINITY ? s : s * exp_of(a, m - z_max));
+            z_sum = lanes_reduce<Sum, 64>(lane < a.parts ? relative(a, Running{m, s}, z_max) : 0.f);
         } else {
             z_max = a.row_max[p.r];
             z_sum = a.row_sum[p.r];
@@ -418,29 +439,20 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
             const float g = (a.row_weight ? a.row_weight[p.r] : 1.f) * a.temperature, g_q = g / z_sum;
             const bool none = !some || g == 0.f;
             const size_t d0 = p.r * a.ld_dlogits;
-            float v[N];
-            auto put = [&](u32x4 raw, size_t c, uint32_t left) {
-                unpack<DT>(raw, v);
+            auto taken = [&](u32x4 chunk) { return none ? u32x4{0u, 0u, 0u, 0u} : pull<DT>(a, chunk, z_max, g_q); };
+            for (uint32_t c0 = p.begin; c0 < p.end;) {
 #pragma unroll
-                for (int e = 0; e < N; e++)
-                    v[e] = none ? 0.f : exp_of(a, v[e] - z_max) * g_q;
-                store_chunk<DT>(a.dlogits, d0 + c * N, left, pack<DT>(v));
-            };
-            for (uint32_t c0 = p.begin + threadIdx.x; c0 < p.end; c0 += P * kSlice) {
-                u32x4 raw[P];
-#pragma unroll
-                for (int i = 0; i < P; i++) {
-                    raw[i] = u32x4{0u, 0u, 0u, 0u};
-                    if (c0 + (uint32_t)i * kSlice < p.end)
-                        raw[i] = load_chunk<DT>(a.logits, z0 + (size_t)(c0 + (uint32_t)i * kSlice) * N, N);
+                for (int i = 0; i < kAhead; i++) {
+                    const uint32_t c = c0 + threadIdx.x + (uint32_t)i * kSlice;
+                    if (c < p.end)
+                        store_whole<DT>((unsigned char *)a.dlogits + d0 * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u, taken(raw[i]));
                 }
-#pragma unroll
-                for (int i = 0; i < P; i++)
-                    if (c0 + (uint32_t)i * kSlice < p.end)
-                        put(raw[i], c0 + (uint32_t)i * kSlice, N);
+                c0 += kAhead * kSlice;
+                if (c0 < p.end)
+                    fetch<DT>(a, p, c0, raw);
             }
             if (a.tail && p.last && threadIdx.x == 0)
-                put(load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail), a.full, a.tail);
+                store_chunk<DT>(a.dlogits, d0 + (size_t)a.full * N, a.tail, taken(load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail)));
             __syncthreads();
             const bool repeats = a.k && *list.repeats != 0;
             for (uint32_t j = threadIdx.x; j < a.k && !none; j += kSlice) {
@@ -463,9 +475,9 @@ struct RowKernel {
 };
 
 #define ROW_KERNEL(T, P) {T, T * P, {distill_row_kernel<kF32, T, P>, distill_row_kernel<kBF16, T, P>}}
-static const RowKernel kRowKernels[] = {ROW_KERNEL(64, 4), ROW_KERNEL(64, 16), ROW_KERNEL(256, 8), ROW_KERNEL(256, 16), ROW_KERNEL(512, 16), ROW_KERNEL(1024, 16)};
+static const RowKernel kRowKernels[] = {ROW_KERNEL(64, 4), ROW_KERNEL(64, 16), ROW_KERNEL(256, 8), ROW_KERNEL(256, 16), ROW_KERNEL(512, 16), ROW_KERNEL(512, 32), ROW_KERNEL(512, 48)};
 #undef ROW_KERNEL
-constexpr uint32_t kHeld = 1024 * 16;
+constexpr uint32_t kHeld = 512 * 48;
 
 // How a call is cut: parts = 0 is a row per workgroup.
 struct Cut {
@@ -490,7 +502,7 @@ static Cut cut_loss(int64_t rows, int64_t vocab, tmask_dtype dt)
     const uint32_t chunks = (uint32_t)(vocab / (dt == TMASK_F32 ? 4 : 8));
     if (chunks <= 1024 || (rows >= 256 && chunks <= kHeld))
         return {0, 0};
-    return cut_rows(rows, chunks, 512, 4096);
+    return cut_rows(rows, chunks, 512, kAhead * kSlice);
 }
 
 static uint32_t grid_of(uint64_t workgroups) { return (uint32_t)(workgroups < (1u << 20) ? workgroups : 1u << 20); }
@@ -593,7 +605,7 @@ extern "C" int tmask_distill_backward(const tmask_distill_desc *desc, tmask_dtyp
     TMASK_TRY(check_vector("row_max", desc->row_max, 4, true));
     TMASK_TRY(check_vector("row_sum", desc->row_sum, 4, true));
     TMASK_TRY(check_rows("dlogits", desc->dlogits, desc->ld_dlogits, desc->rows, desc->vocab, size_of(dt), true));
-    const Cut cut = cut_rows(desc->rows, a.full, 512, 8192);
+    const Cut cut = cut_rows(desc->rows, a.full, 512, kAhead * kSlice);
     a.parts = cut.parts;
     a.part_chunks = cut.part_chunks;
     hipLaunchKernelGGL((dt == TMASK_BF16 ? distill_slice_kernel<kBF16, false> : distill_slice_kernel<kF32, false>),

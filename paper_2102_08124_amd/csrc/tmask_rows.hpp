@@ -59,6 +59,25 @@ __device__ __forceinline__ u32x4 load_chunk(const void *p, size_t i, uint32_t le
     return v;
 }
 
+// A whole chunk at `offset` bytes from an address that is the same for the wavefront, which then is held in scalar registers.
+template <int DT>
+__device__ __forceinline__ u32x4 load_whole(const unsigned char *p, uint32_t offset)
+{
+    if constexpr (DT == kF32)
+        return *(const u32x4_at4 *)(p + offset);
+    else
+        return *(const u32x4_at2 *)(p + offset);
+}
+
+template <int DT>
+__device__ __forceinline__ void store_whole(unsigned char *p, uint32_t offset, u32x4 raw)
+{
+    if constexpr (DT == kF32)
+        *(u32x4_at4 *)(p + offset) = raw;
+    else
+        *(u32x4_at2 *)(p + offset) = raw;
+}
+
 template <int DT>
 __device__ __forceinline__ void unpack(u32x4 raw, float (&v)[kElems<DT>])
 {
