@@ -55,16 +55,38 @@ static size_t list_bytes(uint32_t k, uint32_t hash_shift) { return 4u * (4u + 3u
 // exp(x / T) for x <= 0
 __device__ __forceinline__ float exp_of(const DistillArgs &a, float x) { return __builtin_amdgcn_exp2f(x * a.per_t2); }
 
-// Entry j of row r, written to the list; the result is its logit if it counts, +Inf for NaN, else -Inf.
-__device__ __forceinline__ float read_entry(const DistillArgs &a, uint32_t r, uint32_t j, const List &l)
+constexpr int kEntries = 4;               // that a thread reads at a time
+
+// Entry j of row r as it lies in memory: nothing is computed from it here, so that a thread's loads are all in flight at once.
+struct Entry {
+    uint32_t t, lo, hi;
+};
+
+__device__ __forceinline__ Entry entry_at(const DistillArgs &a, uint32_t r, uint32_t j)
 {
     const size_t i = r * a.ld_index + j, k = r * a.ld_teacher + j;
-    const int64_t at = a.index64 ? ((const int64_t *)a.index)[i] : (int64_t)((const int32_t *)a.index)[i];
-    const float t = a.teacher_f32 ? load_one<kF32>(a.teacher, k) : load_one<kBF16>(a.teacher, k);
-    const bool counts = at >= 0 && at < (int64_t)a.vocab && t != -INFINITY;
-    l.at[j] = counts ? (int32_t)at : -1;
-    l.t[j] = t;
-    return !counts ? -INFINITY : t != t ? INFINITY : t;
+    Entry e;
+    e.hi = 0;
+    if (a.index64) {
+        const u32x2 at = *(const u32x2 *)((const uint64_t *)a.index + i);
+        e.lo = at.x;
+        e.hi = at.y;
+    } else {
+        e.lo = ((const uint32_t *)a.index)[i];
+    }
+    if (a.teacher_f32)
+        e.t = ((const uint32_t *)a.teacher)[k];
+    else
+        e.t = ((const uint16_t *)a.teacher)[k];
+    return e;
+}
+
+__device__ __forceinline__ float logit_of(const DistillArgs &a, const Entry &e) { return __uint_as_float(a.teacher_f32 ? e.t : e.t << 16); }
+
+// its column, -1 if it does not count (below 2^31 with the upper half 0, so one unsigned comparison sees negative indexes too)
+__device__ __forceinline__ int32_t column_of(const DistillArgs &a, const Entry &e)
+{
+    return e.hi == 0 && e.lo < a.vocab && logit_of(a, e) != -INFINITY ? (int32_t)e.lo : -1;
 }
 
 // Notes whether `at` has been entered before.  The table has at least twice as many places as the list has entries, so the search
@@ -83,6 +105,44 @@ __device__ __forceinline__ void enter(const DistillArgs &a, const List &l, int32
         }
         h = (h + 1u) & mask;
     }
+}
+
+// Reads row r's list into LDS; as_logit(logit(at, j)): the student's logit of entry j, loaded and made fp32; noted(at): whether
+// repeats of that column matter.  The result is the thread's largest logit of an entry (+Inf for NaN), -Inf if it has none.
+template <uint32_t T, typename Logit, typename AsLogit, typename Noted>
+__device__ __forceinline__ float read_list(const DistillArgs &a, uint32_t r, const List &l, Logit logit, AsLogit as_logit, Noted noted)
+{
+    float t_max = -INFINITY;
+    for (uint32_t j0 = threadIdx.x; j0 < a.k; j0 += kEntries * T) {
+        Entry e[kEntries];
+        int32_t at[kEntries];
+        decltype(logit(0, 0u)) z[kEntries];
+#pragma unroll
+        for (int i = 0; i < kEntries; i++)
+            if (j0 + (uint32_t)i * T < a.k)
+                e[i] = entry_at(a, r, j0 + (uint32_t)i * T);
+#pragma unroll
+        for (int i = 0; i < kEntries; i++) {
+            at[i] = j0 + (uint32_t)i * T < a.k ? column_of(a, e[i]) : -1;
+            if (at[i] >= 0)
+                z[i] = logit(at[i], j0 + (uint32_t)i * T);
+        }
+#pragma unroll
+        for (int i = 0; i < kEntries; i++) {
+            const uint32_t j = j0 + (uint32_t)i * T;
+            if (j < a.k)
+                l.at[j] = at[i];
+            if (at[i] >= 0) {
+                const float t = logit_of(a, e[i]);
+                l.t[j] = t;
+                l.z[j] = as_logit(z[i]);
+                t_max = fmaxf(t_max, t != t ? INFINITY : t);
+                if (noted(at[i]))
+                    enter(a, l, at[i]);
+            }
+        }
+    }
+    return t_max;
 }
 
 template <uint32_t T>
@@ -181,12 +241,13 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
         const size_t z0 = r * a.ld_logits;
         u32x4 raw[P / G][G], last[1] = {no_chunk<DT>()};
         const bool has_last = a.tail && threadIdx.x == 0;
+        const float g = a.dlogits ? (a.row_weight ? a.row_weight[r] : 1.f) * a.temperature : 0.f;
 #pragma unroll
         for (int i = 0; i < P; i++) {
             const uint32_t c = threadIdx.x + (uint32_t)(i * T);
             raw[i / G][i % G] = no_chunk<DT>();
             if (c < a.full)
-                raw[i / G][i % G] = load_whole<DT>((const unsigned char *)a.logits + z0 * kSize<DT> + (size_t)(i * T) * 16u, threadIdx.x * 16u);
+                raw[i / G][i % G] = load_whole<DT, true>((const unsigned char *)a.logits + z0 * kSize<DT> + (size_t)(i * T) * 16u, threadIdx.x * 16u);
         }
         if (has_last)
             last[0] = load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail, -INFINITY);
@@ -194,15 +255,8 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
         if (a.k) {
             clear_table<T>(a, list);
             __syncthreads();
-            for (uint32_t j = threadIdx.x; j < a.k; j += T) {
-                t_max = fmaxf(t_max, read_entry(a, r, j, list));
-                const int32_t at = list.at[j];
-                if (at >= 0) {
-                    list.z[j] = load_one<DT>(a.logits, z0 + (uint32_t)at);
-                    if (a.dlogits)
-                        enter(a, list, at);
-                }
-            }
+            t_max = read_list<T>(a, r, list, [&](int32_t at, uint32_t) { return load_bits<DT>(a.logits, z0 + (uint32_t)at); }, from_bits<DT>,
+                                 [&](int32_t) { return a.dlogits != nullptr; });
         }
         Running run = {-INFINITY, 0.f};
 #pragma unroll
@@ -233,7 +287,6 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
         if ((threadIdx.x & 63) == 0)
             red[4 * W + (threadIdx.x >> 6)] = loss;
 
-        const float g = a.dlogits ? (a.row_weight ? a.row_weight[r] : 1.f) * a.temperature : 0.f;
         const float g_q = g / z_sum;
         const bool none = !some || g == 0.f;
         const size_t d0 = r * a.ld_dlogits;
@@ -242,7 +295,7 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
             for (int i = 0; i < P; i++) {
                 const uint32_t c = threadIdx.x + (uint32_t)(i * T);
                 if (c < a.full)
-                    store_whole<DT>((unsigned char *)a.dlogits + d0 * kSize<DT> + (size_t)(i * T) * 16u, threadIdx.x * 16u,
+                    store_whole<DT, true>((unsigned char *)a.dlogits + d0 * kSize<DT> + (size_t)(i * T) * 16u, threadIdx.x * 16u,
                                     none ? u32x4{0u, 0u, 0u, 0u} : pull<DT>(a, raw[i / G][i % G], z_max, g_q));
             }
             if (has_last)
@@ -303,7 +356,7 @@ __device__ __forceinline__ bool in_part(const DistillArgs &a, const Part &p, int
     return at >= 0 && (uint32_t)at >= p.begin * N && (p.last || (uint32_t)at < p.end * N);
 }
 
-template <int DT>
+template <int DT, bool STREAM>
 __device__ __forceinline__ void fetch(const DistillArgs &a, const Part &p, uint32_t c0, u32x4 (&raw)[kAhead])
 {
 #pragma unroll
@@ -311,7 +364,7 @@ __device__ __forceinline__ void fetch(const DistillArgs &a, const Part &p, uint3
         const uint32_t c = c0 + threadIdx.x + (uint32_t)i * kSlice;
         raw[i] = no_chunk<DT>();
         if (c < p.end)
-            raw[i] = load_whole<DT>((const unsigned char *)a.logits + p.r * a.ld_logits * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u);
+            raw[i] = load_whole<DT, STREAM>((const unsigned char *)a.logits + p.r * a.ld_logits * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u);
     }
 }
 
@@ -326,7 +379,7 @@ __global__ void __launch_bounds__(kSlice) distill_part_kernel(const DistillArgs 
         Running run = {-INFINITY, 0.f};
         for (uint32_t c0 = p.begin; c0 < p.end; c0 += kAhead * kSlice) {
             u32x4 raw[kAhead];
-            fetch<DT>(a, p, c0, raw);
+            fetch<DT, false>(a, p, c0, raw);
             add_chunks<DT, kAhead>(a, run, raw);
         }
         if (a.tail && p.last && threadIdx.x == 0) {
@@ -367,7 +420,8 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
         const size_t z0 = p.r * a.ld_logits;
         u32x4 raw[kAhead];
         if (a.dlogits)
-            fetch<DT>(a, p, p.begin, raw);
+            fetch<DT, true>(a, p, p.begin, raw);
+        const float g = a.dlogits ? (a.row_weight ? a.row_weight[p.r] : 1.f) * a.temperature : 0.f;
         float z_max, z_sum;
         if constexpr (JOIN) {
             const uint32_t lane = threadIdx.x & 63;
@@ -388,18 +442,15 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
                 clear_table<kSlice>(a, list);
                 __syncthreads();
             }
-            for (uint32_t j = threadIdx.x; j < a.k; j += kSlice) {
-                t_max = fmaxf(t_max, read_entry(a, p.r, j, list));
-                const int32_t at = list.at[j];
-                if (JOIN && at >= 0)
-                    list.z[j] = a.list_logits[(size_t)p.r * a.k + j];
-                if (in_part<DT>(a, p, at)) {
-                    if constexpr (!JOIN)
-                        list.z[j] = load_one<DT>(a.logits, z0 + (uint32_t)at);
-                    if (a.dlogits)
-                        enter(a, list, at);
-                }
-            }
+            t_max = read_list<kSlice>(a, p.r, list,
+                                      [&](int32_t at, uint32_t j) {
+                                          if constexpr (JOIN)
+                                              return __float_as_uint(a.list_logits[(size_t)p.r * a.k + j]);
+                                          else
+                                              return load_bits<DT>(a.logits, z0 + (uint32_t)(in_part<DT>(a, p, at) ? at : 0));
+                                      },
+                                      [](uint32_t bits) { return JOIN ? __uint_as_float(bits) : from_bits<DT>(bits); },
+                                      [&](int32_t at) { return a.dlogits && in_part<DT>(a, p, at); });
         }
         group_reduce<Max, Max, W>(t_max, unused, red);
         for (uint32_t j = threadIdx.x; j < a.k; j += kSlice)
@@ -436,7 +487,7 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
             }
         }
         if (a.dlogits) {
-            const float g = (a.row_weight ? a.row_weight[p.r] : 1.f) * a.temperature, g_q = g / z_sum;
+            const float g_q = g / z_sum;
             const bool none = !some || g == 0.f;
             const size_t d0 = p.r * a.ld_dlogits;
             auto taken = [&](u32x4 chunk) { return none ? u32x4{0u, 0u, 0u, 0u} : pull<DT>(a, chunk, z_max, g_q); };
@@ -445,11 +496,11 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
                 for (int i = 0; i < kAhead; i++) {
                     const uint32_t c = c0 + threadIdx.x + (uint32_t)i * kSlice;
                     if (c < p.end)
-                        store_whole<DT>((unsigned char *)a.dlogits + d0 * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u, taken(raw[i]));
+                        store_whole<DT, true>((unsigned char *)a.dlogits + d0 * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u, taken(raw[i]));
                 }
                 c0 += kAhead * kSlice;
                 if (c0 < p.end)
-                    fetch<DT>(a, p, c0, raw);
+                    fetch<DT, true>(a, p, c0, raw);
             }
             if (a.tail && p.last && threadIdx.x == 0)
                 store_chunk<DT>(a.dlogits, d0 + (size_t)a.full * N, a.tail, taken(load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail)));

@@ -1,5 +1,7 @@
 // What the row kernels (layer norm, bias + GELU, distillation) share: rows in chunks of 16 bytes, sums over lanes and workgroups.
 #pragma once
+#include <type_traits>
+
 #include "tmask_device.hpp"
 
 namespace tmask {
@@ -22,6 +24,22 @@ __device__ __forceinline__ float load_one(const void *p, size_t i)
         return ((const float *)p)[i];
     else
         return __uint_as_float((uint32_t)((const uint16_t *)p)[i] << 16);
+}
+
+// the same in two steps: a loop of loads, and what is computed from them
+template <int DT>
+__device__ __forceinline__ uint32_t load_bits(const void *p, size_t i)
+{
+    if constexpr (DT == kF32)
+        return ((const uint32_t *)p)[i];
+    else
+        return ((const uint16_t *)p)[i];
+}
+
+template <int DT>
+__device__ __forceinline__ float from_bits(uint32_t bits)
+{
+    return __uint_as_float(DT == kF32 ? bits : bits << 16);
 }
 
 // rounded to nearest even
@@ -60,22 +78,27 @@ __device__ __forceinline__ u32x4 load_chunk(const void *p, size_t i, uint32_t le
 }
 
 // A whole chunk at `offset` bytes from an address that is the same for the wavefront, which then is held in scalar registers.
-template <int DT>
+// STREAM: with the non-temporal hint, for what is read or written once and does not fit the caches.
+template <int DT, bool STREAM = false>
 __device__ __forceinline__ u32x4 load_whole(const unsigned char *p, uint32_t offset)
 {
-    if constexpr (DT == kF32)
-        return *(const u32x4_at4 *)(p + offset);
+    typedef std::conditional_t<DT == kF32, u32x4_at4, u32x4_at2> chunk;
+    const chunk *const a = (const chunk *)(p + offset);
+    if constexpr (STREAM)
+        return __builtin_nontemporal_load(a);
     else
-        return *(const u32x4_at2 *)(p + offset);
+        return *a;
 }
 
-template <int DT>
+template <int DT, bool STREAM = false>
 __device__ __forceinline__ void store_whole(unsigned char *p, uint32_t offset, u32x4 raw)
 {
-    if constexpr (DT == kF32)
-        *(u32x4_at4 *)(p + offset) = raw;
+    typedef std::conditional_t<DT == kF32, u32x4_at4, u32x4_at2> chunk;
+    chunk *const a = (chunk *)(p + offset);
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(raw, a);
     else
-        *(u32x4_at2 *)(p + offset) = raw;
+        *a = raw;
 }
 
 template <int DT>
