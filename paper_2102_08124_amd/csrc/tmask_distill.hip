@@ -24,7 +24,6 @@ struct DistillArgs {
     float *list_logits;                   // rows x k: the student's logits of the entries
     size_t ld_logits, ld_teacher, ld_index, ld_dlogits;
     uint32_t rows, vocab, k;
-    uint32_t full, tail;                  // chunks of a row, and the elements behind them (fewer than a chunk's)
     uint32_t parts, part_chunks;
     uint32_t teacher_f32, index64;
     uint32_t hash_shift;
@@ -203,6 +202,45 @@ __device__ __forceinline__ float relative(const DistillArgs &a, Running run, flo
     return run.max == -INFINITY && max != -INFINITY ? run.sum : run.sum * exp_of(a, run.max - max);
 }
 
+// A row as its chunks lie: from the first multiple of 16 bytes on, so that loads are aligned (and stores, if the gradient's rows lie
+// alike: 1003 rows of 50021 bf16 take 52 us with chunks from the row's first element on, 42 like this).  The elements before and behind, up
+// to a chunk less one each, are taken one by one by the first threads of the workgroup that has that end of the row.
+struct RowShape {
+    uint32_t head, full, tail;
+};
+
+template <int DT>
+__device__ __forceinline__ RowShape shape_of(const DistillArgs &a, uint32_t r)
+{
+    constexpr uint32_t N = kElems<DT>;
+    const uint64_t from = (uint64_t)(uintptr_t)a.logits / kSize<DT> + r * (uint64_t)a.ld_logits;
+    RowShape s;
+    s.head = (uint32_t)(0 - from) % N;
+    s.head = s.head < a.vocab ? s.head : a.vocab;
+    s.full = (a.vocab - s.head) / N;
+    s.tail = (a.vocab - s.head) % N;
+    return s;
+}
+
+// The single element of this thread, of `head` at the row's start and `tail` at its end.
+struct Edge {
+    bool there;
+    uint32_t at;
+};
+
+__device__ __forceinline__ Edge edge_of(const DistillArgs &a, uint32_t head, uint32_t tail)
+{
+    return {threadIdx.x < head + tail, threadIdx.x < head ? threadIdx.x : a.vocab - (head + tail) + threadIdx.x};
+}
+
+__device__ __forceinline__ Running start(const DistillArgs &a, Edge edge, float z)
+{
+    if (!edge.there)
+        return {-INFINITY, 0.f};
+    const float m = fmaxf(-INFINITY, z);
+    return {m, exp_of(a, z - (m == -INFINITY ? 0.f : m))};
+}
+
 template <int DT>
 __device__ __forceinline__ u32x4 no_chunk()
 {
@@ -225,7 +263,7 @@ __device__ __forceinline__ u32x4 pull(const DistillArgs &a, u32x4 raw, float z_m
 
 // ---------------------------------------------------------------------------------------------------------------------
 // A row in the registers of one workgroup: T threads with P chunks each.  The logits are read once, added up as they arrive, and the
-// gradient is taken from the registers.  (The chunk that a row ends inside, if its length is odd, is thread 0's.)
+// gradient is taken from the registers.
 //
 // The gradient's columns that the list names are written again, with what the teacher takes from them, when the rest has been
 // written: k of the vocabulary's columns, and the barrier between orders the two.
@@ -233,24 +271,24 @@ __device__ __forceinline__ u32x4 pull(const DistillArgs &a, u32x4 raw, float z_m
 template <int DT, int T, int P>
 __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
 {
-    constexpr int N = kElems<DT>, W = T / 64, G = 4;
+    constexpr int W = T / 64, G = 4;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     float *const red = (float *)lds;                                            // 2 x 2 W numbers, and W
     const List list = list_in(red + 5 * W, a);
     for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const size_t z0 = r * a.ld_logits;
-        u32x4 raw[P / G][G], last[1] = {no_chunk<DT>()};
-        const bool has_last = a.tail && threadIdx.x == 0;
+        const RowShape row = shape_of<DT>(a, r);
+        const Edge edge = edge_of(a, row.head, row.tail);
+        const uint32_t edge_bits = edge.there ? load_bits<DT>(a.logits, z0 + edge.at) : 0u;
+        u32x4 raw[P / G][G];
         const float g = a.dlogits ? (a.row_weight ? a.row_weight[r] : 1.f) * a.temperature : 0.f;
 #pragma unroll
         for (int i = 0; i < P; i++) {
             const uint32_t c = threadIdx.x + (uint32_t)(i * T);
             raw[i / G][i % G] = no_chunk<DT>();
-            if (c < a.full)
-                raw[i / G][i % G] = load_whole<DT, true>((const unsigned char *)a.logits + z0 * kSize<DT> + (size_t)(i * T) * 16u, threadIdx.x * 16u);
+            if (c < row.full)
+                raw[i / G][i % G] = load_whole<DT, true>((const unsigned char *)a.logits + (z0 + row.head) * kSize<DT> + (size_t)(i * T) * 16u, threadIdx.x * 16u);
         }
-        if (has_last)
-            last[0] = load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail, -INFINITY);
         float t_max = -INFINITY;
         if (a.k) {
             clear_table<T>(a, list);
@@ -258,13 +296,12 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
             t_max = read_list<T>(a, r, list, [&](int32_t at, uint32_t) { return load_bits<DT>(a.logits, z0 + (uint32_t)at); }, from_bits<DT>,
                                  [&](int32_t) { return a.dlogits != nullptr; });
         }
-        Running run = {-INFINITY, 0.f};
+        const float single = from_bits<DT>(edge_bits);
+        Running run = start(a, edge, single);
 #pragma unroll
         for (int i = 0; i < P / G; i++)
-            if ((uint32_t)(i * G * T) < a.full)
+            if ((uint32_t)(i * G * T) < row.full)
                 add_chunks<DT, G>(a, run, raw[i]);
-        if (has_last)
-            add_chunks<DT, 1>(a, run, last);
         float z_max = run.max;
         group_reduce<Max, Max, W>(t_max, z_max, red);
         float t_sum = 0.f, z_sum = relative(a, run, z_max);
@@ -291,15 +328,16 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
         const bool none = !some || g == 0.f;
         const size_t d0 = r * a.ld_dlogits;
         if (a.dlogits) {
+            uint32_t me = threadIdx.x;                                          // so that neither the loads' addresses nor their masks are kept until here
+            asm volatile("" : "+v"(me));
 #pragma unroll
             for (int i = 0; i < P; i++) {
-                const uint32_t c = threadIdx.x + (uint32_t)(i * T);
-                if (c < a.full)
-                    store_whole<DT, true>((unsigned char *)a.dlogits + d0 * kSize<DT> + (size_t)(i * T) * 16u, threadIdx.x * 16u,
-                                    none ? u32x4{0u, 0u, 0u, 0u} : pull<DT>(a, raw[i / G][i % G], z_max, g_q));
+                if (me + (uint32_t)(i * T) < row.full)
+                    store_whole<DT, true>((unsigned char *)a.dlogits + (d0 + row.head) * kSize<DT> + (size_t)(i * T) * 16u, me * 16u,
+                                          none ? u32x4{0u, 0u, 0u, 0u} : pull<DT>(a, raw[i / G][i % G], z_max, g_q));
             }
-            if (has_last)
-                store_chunk<DT>(a.dlogits, d0 + (size_t)a.full * N, a.tail, none ? u32x4{0u, 0u, 0u, 0u} : pull<DT>(a, last[0], z_max, g_q));
+            if (edge.there)
+                store_one<DT>(a.dlogits, d0 + edge.at, none ? 0.f : exp_of(a, single - z_max) * g_q);
         }
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -334,27 +372,31 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
 constexpr int kAhead = 8;                 // chunks that a thread has in flight
 
 struct Part {
-    uint32_t r, part, begin, end;         // row, part, chunks
-    bool last;                            // the row's last part: the elements behind the chunks are its own
+    uint32_t r, part;
+    uint32_t begin, end;                  // chunks
+    uint32_t first, behind;               // columns, with the elements before and behind the chunks at the row's ends
+    RowShape row;
+    Edge edge;
 };
 
+template <int DT>
 __device__ __forceinline__ Part part_of(const DistillArgs &a, uint64_t id)
 {
+    constexpr uint32_t N = kElems<DT>;
     Part p;
     p.r = (uint32_t)(id / a.parts);
     p.part = (uint32_t)(id % a.parts);
+    p.row = shape_of<DT>(a, p.r);
+    const bool last = p.part + 1u == a.parts;
     p.begin = p.part * a.part_chunks;
-    p.last = p.part + 1u == a.parts;
-    p.end = p.last ? a.full : p.begin + a.part_chunks;
+    p.end = last ? p.row.full : p.begin + a.part_chunks;
+    p.first = p.part ? p.row.head + p.begin * N : 0u;
+    p.behind = last ? a.vocab : p.row.head + p.end * N;
+    p.edge = edge_of(a, p.part ? 0u : p.row.head, last ? p.row.tail : 0u);
     return p;
 }
 
-template <int DT>
-__device__ __forceinline__ bool in_part(const DistillArgs &a, const Part &p, int32_t at)
-{
-    constexpr uint32_t N = kElems<DT>;
-    return at >= 0 && (uint32_t)at >= p.begin * N && (p.last || (uint32_t)at < p.end * N);
-}
+__device__ __forceinline__ bool in_part(const Part &p, int32_t at) { return at >= 0 && (uint32_t)at >= p.first && (uint32_t)at < p.behind; }
 
 template <int DT, bool STREAM>
 __device__ __forceinline__ void fetch(const DistillArgs &a, const Part &p, uint32_t c0, u32x4 (&raw)[kAhead])
@@ -364,27 +406,23 @@ __device__ __forceinline__ void fetch(const DistillArgs &a, const Part &p, uint3
         const uint32_t c = c0 + threadIdx.x + (uint32_t)i * kSlice;
         raw[i] = no_chunk<DT>();
         if (c < p.end)
-            raw[i] = load_whole<DT, STREAM>((const unsigned char *)a.logits + p.r * a.ld_logits * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u);
+            raw[i] = load_whole<DT, STREAM>((const unsigned char *)a.logits + (p.r * a.ld_logits + p.row.head) * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u);
     }
 }
 
 template <int DT>
 __global__ void __launch_bounds__(kSlice) distill_part_kernel(const DistillArgs a)
 {
-    constexpr int N = kElems<DT>, W = kSlice / 64;
+    constexpr int W = kSlice / 64;
     __shared__ float red[4 * W];
     for (uint64_t id = blockIdx.x; id < (uint64_t)a.rows * a.parts; id += gridDim.x) {
-        const Part p = part_of(a, id);
+        const Part p = part_of<DT>(a, id);
         const size_t z0 = p.r * a.ld_logits;
-        Running run = {-INFINITY, 0.f};
+        Running run = start(a, p.edge, p.edge.there ? load_one<DT>(a.logits, z0 + p.edge.at) : 0.f);
         for (uint32_t c0 = p.begin; c0 < p.end; c0 += kAhead * kSlice) {
             u32x4 raw[kAhead];
             fetch<DT, false>(a, p, c0, raw);
             add_chunks<DT, kAhead>(a, run, raw);
-        }
-        if (a.tail && p.last && threadIdx.x == 0) {
-            u32x4 last[1] = {load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail, -INFINITY)};
-            add_chunks<DT, 1>(a, run, last);
         }
         float all = run.max, unused = 0.f;
         group_reduce<Max, Max, W>(all, unused, red);
@@ -397,7 +435,7 @@ __global__ void __launch_bounds__(kSlice) distill_part_kernel(const DistillArgs 
         for (uint32_t j = threadIdx.x; j < a.k; j += kSlice) {
             const size_t i = p.r * a.ld_index + j;
             const int64_t at = a.index64 ? ((const int64_t *)a.index)[i] : (int64_t)((const int32_t *)a.index)[i];
-            if (at < (int64_t)a.vocab && in_part<DT>(a, p, at < 0 ? -1 : (int32_t)at))
+            if (at < (int64_t)a.vocab && in_part(p, at < 0 ? -1 : (int32_t)at))
                 a.list_logits[(size_t)p.r * a.k + j] = load_one<DT>(a.logits, z0 + (size_t)at);
         }
         if (id + gridDim.x < (uint64_t)a.rows * a.parts)
@@ -409,15 +447,16 @@ __global__ void __launch_bounds__(kSlice) distill_part_kernel(const DistillArgs 
 template <int DT, bool JOIN>
 __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs a)
 {
-    constexpr int N = kElems<DT>, W = kSlice / 64;
+    constexpr int W = kSlice / 64;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     float *const red = (float *)lds;
     const List list = list_in(red + 5 * W, a);
     for (uint64_t id = blockIdx.x; id < (uint64_t)a.rows * a.parts; id += gridDim.x) {
-        const Part p = part_of(a, id);
+        const Part p = part_of<DT>(a, id);
         if (JOIN && !a.dlogits && p.part)                                       // the loss alone is joined by one workgroup a row
             continue;
         const size_t z0 = p.r * a.ld_logits;
+        const uint32_t edge_bits = a.dlogits && p.edge.there ? load_bits<DT>(a.logits, z0 + p.edge.at) : 0u;
         u32x4 raw[kAhead];
         if (a.dlogits)
             fetch<DT, true>(a, p, p.begin, raw);
@@ -447,10 +486,10 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
                                           if constexpr (JOIN)
                                               return __float_as_uint(a.list_logits[(size_t)p.r * a.k + j]);
                                           else
-                                              return load_bits<DT>(a.logits, z0 + (uint32_t)(in_part<DT>(a, p, at) ? at : 0));
+                                              return load_bits<DT>(a.logits, z0 + (uint32_t)(in_part(p, at) ? at : 0));
                                       },
                                       [](uint32_t bits) { return JOIN ? __uint_as_float(bits) : from_bits<DT>(bits); },
-                                      [&](int32_t at) { return a.dlogits && in_part<DT>(a, p, at); });
+                                      [&](int32_t at) { return a.dlogits && in_part(p, at); });
         }
         group_reduce<Max, Max, W>(t_max, unused, red);
         for (uint32_t j = threadIdx.x; j < a.k; j += kSlice)
@@ -496,19 +535,19 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
                 for (int i = 0; i < kAhead; i++) {
                     const uint32_t c = c0 + threadIdx.x + (uint32_t)i * kSlice;
                     if (c < p.end)
-                        store_whole<DT, true>((unsigned char *)a.dlogits + d0 * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u, taken(raw[i]));
+                        store_whole<DT, true>((unsigned char *)a.dlogits + (d0 + p.row.head) * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u, taken(raw[i]));
                 }
                 c0 += kAhead * kSlice;
                 if (c0 < p.end)
                     fetch<DT, true>(a, p, c0, raw);
             }
-            if (a.tail && p.last && threadIdx.x == 0)
-                store_chunk<DT>(a.dlogits, d0 + (size_t)a.full * N, a.tail, taken(load_chunk<DT>(a.logits, z0 + (size_t)a.full * N, a.tail)));
+            if (p.edge.there)
+                store_one<DT>(a.dlogits, d0 + p.edge.at, none ? 0.f : exp_of(a, from_bits<DT>(edge_bits) - z_max) * g_q);
             __syncthreads();
             const bool repeats = a.k && *list.repeats != 0;
             for (uint32_t j = threadIdx.x; j < a.k && !none; j += kSlice) {
                 const int32_t at = list.at[j];
-                if (in_part<DT>(a, p, at))
+                if (in_part(p, at))
                     store_one<DT>(a.dlogits, d0 + (uint32_t)at, exp_of(a, list.z[j] - z_max) * g_q - g * (repeats ? share_of(a, list, at) : list.t[j]));
             }
         }
@@ -526,7 +565,13 @@ struct RowKernel {
 };
 
 #define ROW_KERNEL(T, P) {T, T * P, {distill_row_kernel<kF32, T, P>, distill_row_kernel<kBF16, T, P>}}
-static const RowKernel kRowKernels[] = {ROW_KERNEL(64, 4), ROW_KERNEL(64, 16), ROW_KERNEL(256, 8), ROW_KERNEL(256, 16), ROW_KERNEL(512, 16), ROW_KERNEL(512, 32), ROW_KERNEL(512, 48)};
+// A compute unit holds several of the smaller workgroups, which overlap one row's loads with another's arithmetic: with many rows they win
+// (2048 rows of 15000 bf16: 256 threads with 8 chunks each 31 us, 1024 with 4 58).  Up to a row for each of 256 compute units nothing
+// overlaps, and a row is done soonest by many threads (64 rows of 8000 bf16: 64 threads with 16 chunks 10.1 us, 1024 with 4 6.8).
+static const RowKernel kManyRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(64, 8), ROW_KERNEL(256, 4), ROW_KERNEL(256, 8), ROW_KERNEL(256, 16), ROW_KERNEL(512, 16),
+                                      ROW_KERNEL(512, 32), ROW_KERNEL(512, 48)};
+static const RowKernel kFewRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(256, 4), ROW_KERNEL(1024, 4), ROW_KERNEL(1024, 8), ROW_KERNEL(512, 32), ROW_KERNEL(512, 48)};
+constexpr int64_t kFew = 256;
 #undef ROW_KERNEL
 constexpr uint32_t kHeld = 512 * 48;
 
@@ -548,10 +593,14 @@ static Cut cut_rows(int64_t rows, uint32_t chunks, uint32_t least, uint32_t most
     return {chunks ? (chunks + size - 1) / size : 1, size};
 }
 
+static uint32_t chunks_of(int64_t vocab, tmask_dtype dt) { return (uint32_t)(vocab / (dt == TMASK_F32 ? 4 : 8)); }   // of a row at most
+
 static Cut cut_loss(int64_t rows, int64_t vocab, tmask_dtype dt)
 {
-    const uint32_t chunks = (uint32_t)(vocab / (dt == TMASK_F32 ? 4 : 8));
-    if (chunks <= 1024 || (rows >= 256 && chunks <= kHeld))
+    const uint32_t chunks = chunks_of(vocab, dt);
+    // A second launch costs 3 us; a row in one workgroup longer, the longer it is and the fewer compute units have one (us, row / parts:
+    // 16 rows of 32000 bf16 8.4 / 10.0, of 64000 11.9 / 10.1; 64 rows of 64000 12.6 / 15.4, of 131072 22.8 / 16.5; 256 rows of 131072 34 both).
+    if (chunks <= 4096 || rows >= (chunks <= 8192 ? 64 : chunks <= kHeld ? kFew : INT64_MAX))
         return {0, 0};
     return cut_rows(rows, chunks, 512, kAhead * kSlice);
 }
@@ -584,8 +633,6 @@ static int check_distill(const tmask_distill_desc *desc, tmask_dtype dt, tmask_d
     a.part_stats = a.list_logits = nullptr;
     a.ld_logits = (size_t)d.ld_logits; a.ld_teacher = (size_t)d.ld_teacher; a.ld_index = (size_t)d.ld_index; a.ld_dlogits = (size_t)d.ld_dlogits;
     a.rows = (uint32_t)d.rows; a.vocab = (uint32_t)d.vocab; a.k = (uint32_t)d.k;
-    const uint32_t n = dt == TMASK_F32 ? 4 : 8;
-    a.full = a.vocab / n; a.tail = a.vocab % n;
     a.parts = a.part_chunks = 0;
     a.teacher_f32 = teacher_dt == TMASK_F32; a.index64 = index_bits == 64;
     a.hash_shift = 31;
@@ -628,8 +675,8 @@ extern "C" int tmask_distill(const tmask_distill_desc *desc, tmask_dtype dt, tma
     const size_t list = list_bytes(a.k, a.hash_shift);
     const bool bf16 = dt == TMASK_BF16;
     if (cut.parts == 0) {
-        const RowKernel *k = kRowKernels;
-        while (k->chunks < a.full)
+        const RowKernel *k = desc->rows <= kFew ? kFewRows : kManyRows;
+        while (k->chunks < chunks_of(desc->vocab, dt))
             k++;
         hipLaunchKernelGGL(k->kernel[bf16], dim3(grid_of(a.rows)), dim3(k->threads), 20 * (k->threads / 64) + list, stream, a);
     } else {
@@ -656,7 +703,7 @@ extern "C" int tmask_distill_backward(const tmask_distill_desc *desc, tmask_dtyp
     TMASK_TRY(check_vector("row_max", desc->row_max, 4, true));
     TMASK_TRY(check_vector("row_sum", desc->row_sum, 4, true));
     TMASK_TRY(check_rows("dlogits", desc->dlogits, desc->ld_dlogits, desc->rows, desc->vocab, size_of(dt), true));
-    const Cut cut = cut_rows(desc->rows, a.full, 512, kAhead * kSlice);
+    const Cut cut = cut_rows(desc->rows, chunks_of(desc->vocab, dt), 512, kAhead * kSlice);
     a.parts = cut.parts;
     a.part_chunks = cut.part_chunks;
     hipLaunchKernelGGL((dt == TMASK_BF16 ? distill_slice_kernel<kBF16, false> : distill_slice_kernel<kF32, false>),
