@@ -95,6 +95,35 @@ __device__ __forceinline__ void load_params(const void *p, uint32_t f32, size_t 
     }
 }
 
+template <int N>
+__device__ __forceinline__ void store_params(void *p, uint32_t f32, size_t c, uint32_t left, const float (&v)[N])
+{
+    if (f32) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4)
+            if ((uint32_t)e < left)
+                store_chunk<kF32>(p, c + e, left - e, pack<kF32>({v[e], v[e + 1], v[e + 2], v[e + 3]}));
+    } else if constexpr (N == 8) {
+        store_chunk<kBF16>(p, c, left, pack<kBF16>(v));
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            if ((uint32_t)e < left)
+                store_one<kBF16>(p, c + e, v[e]);
+    }
+}
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// N sums to 16-byte aligned memory
+template <int N>
+__device__ __forceinline__ void store_sums(float *p, const float (&v)[N])
+{
+#pragma unroll
+    for (int e = 0; e < N; e += 4)
+        *(f32x4 *)(p + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+}
+
 // ---------------------------------------------------------------------------------------------------------------------
 // Layer norm of rows that stay in registers: LANES lanes (a part of a wavefront, or a workgroup of several) with E elements each,
 // in chunks of 16 bytes that alternate between the lanes.  The mean first, then the mean of the squared differences
@@ -268,12 +297,12 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormArgs 
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Its gradients, with rows held the same way.  A workgroup goes through every strips-th group of rows and keeps the sums over
+// Its gradients, with rows held the same way.  A workgroup, one on a compute unit, goes through every strips-th group of rows and keeps the sums over
 // them of dy h and dy in registers, a column in the same lane all the time; at its end the lanes and wavefronts that share
 // a column add up in LDS, and the strips' sums are added up by columns_kernel.  Rows are loaded one ahead.
 // ---------------------------------------------------------------------------------------------------------------------
-template <int LANES>
-constexpr int kNormGradThreads = LANES <= 64 ? 512 : LANES;
+constexpr int kGradThreads = 1024;
+constexpr uint32_t kGradStrips = 256;
 
 // `v` over the lanes of a wavefront with the same number modulo LANES
 template <int LANES>
@@ -292,29 +321,31 @@ __device__ __forceinline__ float across_rows(float v)
     return v;
 }
 
-template <int DT, int LANES, int E>
-__global__ void __launch_bounds__(kNormGradThreads<LANES>) norm_grad_kernel(const NormGradArgs p)
+template <int DT, int LANES, int E, bool KEEP>
+__global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradArgs p)
 {
-    constexpr int T = kNormGradThreads<LANES>, N = kElems<DT>, C = E / N, kRows = T / LANES, W = T / 64, kCols = LANES * E;
+    constexpr int T = kGradThreads, N = kElems<DT>, C = E / N, kRows = T / LANES, W = T / 64, kCols = LANES * E;
+    constexpr int kShared = LANES < 64 ? W : kRows;                             // sets of column sums that the workgroup adds up
     __shared__ float red[2][2 * W];
     const uint32_t lane = threadIdx.x % LANES;
-    float w[E], dw[E], db[E];
+    float w[C][N], dw[C][N], db[C][N];
     uint32_t left[C];
-#pragma unroll
-    for (int i = 0; i < C; i++) {
-        const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
-        left[i] = c >= p.cols ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
-        float v[N];
+    auto weights = [&](int i, float (&v)[N]) {
 #pragma unroll
         for (int e = 0; e < N; e++)
             v[e] = 1.f;
         if (p.weight && left[i])
-            load_params<N>(p.weight, p.param_f32, c, left[i], v);
+            load_params<N>(p.weight, p.param_f32, (lane + (uint32_t)(i * LANES)) * N, left[i], v);
+    };
 #pragma unroll
-        for (int e = 0; e < N; e++) {
-            w[i * N + e] = v[e];
-            dw[i * N + e] = db[i * N + e] = 0.f;
-        }
+    for (int i = 0; i < C; i++) {
+        const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
+        left[i] = c >= p.cols ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
+        if constexpr (KEEP)
+            weights(i, w[i]);
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            dw[i][e] = db[i][e] = 0.f;
     }
     struct Row {
         u32x4 dy[C], x[C], more[C];
@@ -338,11 +369,15 @@ __global__ void __launch_bounds__(kNormGradThreads<LANES>) norm_grad_kernel(cons
     // the same number of rounds for the whole workgroup: barriers are inside
     const uint32_t step = p.strips * kRows;
     uint32_t r = blockIdx.x * kRows + threadIdx.x / LANES, turn = 0;
-    fetch(r, next);
+    if constexpr (KEEP)
+        fetch(r, next);
     for (uint32_t r0 = blockIdx.x * kRows; r0 < p.rows; r0 += step, r += step, turn ^= 1) {
+        if constexpr (!KEEP)
+            fetch(r, next);
         const Row row = next;
-        if (r0 + step < p.rows)
-            fetch(r + step, next);
+        if constexpr (KEEP)
+            if (r0 + step < p.rows)
+                fetch(r + step, next);
         const bool exists = r < p.rows;
         float d[E], h[E], s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -350,23 +385,37 @@ __global__ void __launch_bounds__(kNormGradThreads<LANES>) norm_grad_kernel(cons
             float v[N], u[N];
             unpack<DT>(row.dy[i], v);
             unpack<DT>(row.x[i], u);
+            if constexpr (!KEEP)
+                weights(i, w[i]);
 #pragma unroll
             for (int e = 0; e < N; e++) {
                 const int k = i * N + e;
                 // dy is 0 in columns and rows that do not exist
                 h[k] = (u[e] - row.mean) * row.rstd;
-                dw[k] += v[e] * h[k];
-                db[k] += v[e];
-                d[k] = v[e] * w[k];
+                dw[i][e] += v[e] * h[k];
+                db[i][e] += v[e];
+                d[k] = v[e] * w[i][e];
                 s1 += d[k];
                 s2 += d[k] * h[k];
             }
         }
-        if constexpr (LANES <= 64) {
-            s1 = lanes_reduce<Sum, LANES>(s1);
-            s2 = lanes_reduce<Sum, LANES>(s2);
-        } else {
-            group_reduce<Sum, Sum, W>(s1, s2, red[turn]);
+        s1 = lanes_reduce<Sum, LANES < 64 ? LANES : 64>(s1);
+        s2 = lanes_reduce<Sum, LANES < 64 ? LANES : 64>(s2);
+        if constexpr (LANES > 64) {
+            constexpr uint32_t kWaves = LANES / 64;                             // of a row
+            const uint32_t wave = threadIdx.x >> 6, first = wave / kWaves * kWaves;
+            if ((threadIdx.x & 63) == 0) {
+                red[turn][wave] = s1;
+                red[turn][W + wave] = s2;
+            }
+            __syncthreads();
+            s1 = red[turn][first];
+            s2 = red[turn][W + first];
+#pragma unroll
+            for (uint32_t k = 1; k < kWaves; k++) {
+                s1 += red[turn][first + k];
+                s2 += red[turn][W + first + k];
+            }
         }
         s1 *= p.per_col;
         s2 *= p.per_col;
@@ -383,45 +432,50 @@ __global__ void __launch_bounds__(kNormGradThreads<LANES>) norm_grad_kernel(cons
     }
     if (!p.dweight && !p.dbias)
         return;
-    // (-0, not 0, would be the neutral element of these sums: a sum of no rows but of -0 alone ends as 0)
-    auto put = [&](uint32_t which, uint32_t c, float v) {
-        if (p.strips > 1) {
-            p.partial[((size_t)blockIdx.x * 2 + which) * p.pitch + c] = v;
-        } else {
-            void *const out = which ? p.dbias : p.dweight;
-            if (out)
-                store_param(out, p.param_f32, c, v);
-        }
-    };
     if constexpr (kRows == 1) {
 #pragma unroll
-        for (int k = 0; k < E; k++) {
-            const uint32_t c = (lane + (uint32_t)(k / N * LANES)) * N + (uint32_t)(k % N);
-            if (c < p.cols) {
-                put(0, c, dw[k]);
-                put(1, c, db[k]);
+        for (int i = 0; i < C; i++) {
+            const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
+            if (left[i] && p.strips > 1) {
+                store_sums(p.partial + (size_t)blockIdx.x * 2 * p.pitch + c, dw[i]);
+                store_sums(p.partial + ((size_t)blockIdx.x * 2 + 1) * p.pitch + c, db[i]);
+            } else if (left[i]) {
+                if (p.dweight)
+                    store_params(p.dweight, p.param_f32, c, left[i], dw[i]);
+                if (p.dbias)
+                    store_params(p.dbias, p.param_f32, c, left[i], db[i]);
             }
         }
     } else {
-        __shared__ float sums[W][2][kCols];
+        __shared__ __attribute__((aligned(16))) float sums[kShared][2][kCols];
+        const uint32_t set = LANES < 64 ? threadIdx.x >> 6 : threadIdx.x / LANES;
 #pragma unroll
-        for (int k = 0; k < E; k++) {
-            const float a = across_rows<LANES>(dw[k]), b = across_rows<LANES>(db[k]);
-            const uint32_t c = (lane + (uint32_t)(k / N * LANES)) * N + (uint32_t)(k % N);
-            if ((threadIdx.x & 63) < (uint32_t)LANES) {
-                sums[threadIdx.x >> 6][0][c] = a;
-                sums[threadIdx.x >> 6][1][c] = b;
+        for (int i = 0; i < C; i++) {
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                dw[i][e] = across_rows<LANES>(dw[i][e]);
+                db[i][e] = across_rows<LANES>(db[i][e]);
+            }
+            if (LANES >= 64 || (threadIdx.x & 63) < (uint32_t)LANES) {
+                const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
+                store_sums(&sums[set][0][c], dw[i]);
+                store_sums(&sums[set][1][c], db[i]);
             }
         }
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < 2u * kCols; i += T) {
-            const uint32_t which = i / kCols, c = i % kCols;
+        for (uint32_t k = threadIdx.x; k < 2u * kCols; k += T) {
+            const uint32_t which = k / kCols, c = k % kCols;
             float s = 0.f;
 #pragma unroll
-            for (int k = 0; k < W; k++)
-                s += sums[k][which][c];
-            if (c < p.cols)
-                put(which, c, s);
+            for (int i = 0; i < kShared; i++)
+                s += sums[i][which][c];
+            if (c < p.cols && p.strips > 1) {
+                p.partial[((size_t)blockIdx.x * 2 + which) * p.pitch + c] = s;
+            } else if (c < p.cols) {
+                void *const out = which ? p.dbias : p.dweight;
+                if (out)
+                    store_param(out, p.param_f32, c, s);
+            }
         }
     }
 }
@@ -514,8 +568,9 @@ __device__ __forceinline__ float gelu(float u)
         q = fmaf(q, t, 0.20633404f);
         q = fmaf(q, t, 0.12138055f);
         q *= t * exponential;
-        const float share = u < 0.f ? q : 1.f - q;
-        return GRAD ? fmaf(u * 0.39894228f, exponential, share) : u * share;
+        if constexpr (GRAD)
+            return fmaf(u * 0.39894228f, exponential, u < 0.f ? q : 1.f - q);
+        return fmaf(-a, q, fmaxf(u, 0.f));                    // u q below 0, u - u q above; what is left of a large |u| keeps its digits
     } else {
         const float u2 = fminf(u * u, 1e4f);                  // the share is 0 or 1 long before; the square stays finite
         const float share = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.3022082f * u * fmaf(0.044715f, u2, 1.f)));
@@ -523,15 +578,18 @@ __device__ __forceinline__ float gelu(float u)
     }
 }
 
-// Workgroups of 256 threads as 2^lanes_log2 lanes of a chunk each by the rest of the rows; a thread keeps its columns (and their
+// Workgroups of 256 threads (1024 for gradients, to have fewer strips) as 2^lanes_log2 lanes of a chunk each by the rest of the rows; a thread keeps its columns (and their
 // bias and, for gradients, their sums) and takes kGeluRows rows at a time.
 constexpr int kGeluRows = 4;
 
+template <bool GRAD>
+constexpr int kGeluThreads = GRAD ? kGradThreads : kThreads;
+
 template <int DT, int FORM, bool GRAD>
-__global__ void __launch_bounds__(kThreads) gelu_kernel(const GeluArgs p)
+__global__ void __launch_bounds__(kGeluThreads<GRAD>) gelu_kernel(const GeluArgs p)
 {
-    constexpr int N = kElems<DT>;
-    const uint32_t lanes = 1u << p.lanes_log2, high = kThreads >> p.lanes_log2;
+    constexpr int N = kElems<DT>, T = kGeluThreads<GRAD>;
+    const uint32_t lanes = 1u << p.lanes_log2, high = T >> p.lanes_log2;
     const uint32_t group = blockIdx.x % p.groups, strip = blockIdx.x / p.groups;
     const uint32_t chunk = group * lanes + (threadIdx.x & (lanes - 1u)), y = threadIdx.x >> p.lanes_log2;
     const uint32_t c = chunk * N, left = chunk >= p.chunks ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
@@ -577,12 +635,10 @@ __global__ void __launch_bounds__(kThreads) gelu_kernel(const GeluArgs p)
     if constexpr (GRAD) {
         if (!p.dbias)
             return;
-        __shared__ float sums[kThreads * N];                                    // [y][lane][element]
-#pragma unroll
-        for (int e = 0; e < N; e++)
-            sums[threadIdx.x * N + e] = sum[e];
+        __shared__ __attribute__((aligned(16))) float sums[T * N];               // [y][lane][element]
+        store_sums(sums + threadIdx.x * N, sum);
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < lanes * N; i += kThreads) {
+        for (uint32_t i = threadIdx.x; i < lanes * N; i += T) {
             const uint32_t col = group * lanes * N + i;
             float s = 0.f;
             for (uint32_t k = 0; k < high; k++)
@@ -605,9 +661,8 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(const ColumnArgs p)
         return;
     __shared__ float sums[32][33];
     const uint32_t x = threadIdx.x % 8u, y = threadIdx.x / 8u, c = blockIdx.x * 32u + x * 4u;
-    typedef float f32x4 __attribute__((ext_vector_type(4)));
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    if (c < p.cols)                                                             // the pitch is a multiple of four
+    if (c < p.cols)                                                             // the pitch is a multiple of eight
 #pragma unroll 4
         for (uint32_t k = y; k < p.strips; k += 32u)
             s += *(const f32x4 *)(p.partial + ((size_t)k * p.sums + blockIdx.y) * p.pitch + c);
@@ -629,22 +684,30 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(const ColumnArgs p)
 // ---------------------------------------------------------------------------------------------------------------------
 // How a row is held, by its width.
 struct NormShape {
-    uint32_t cols, rows, grad_rows;                                             // the widest row; rows of a workgroup at a time
-    uint32_t threads, grad_threads;
+    uint32_t cols, rows, threads;                                               // the widest row; rows of a workgroup at a time
     void (*kernel[2])(const NormArgs);
-    void (*grad[2])(const NormGradArgs);
 };
 
-#define NORM_SHAPE(LANES, E)                                                                                        \
-    {LANES * E, kNormThreads<LANES> / LANES, kNormGradThreads<LANES> / LANES, kNormThreads<LANES>, kNormGradThreads<LANES>, \
-     {norm_kernel<kF32, LANES, E>, norm_kernel<kBF16, LANES, E>}, {norm_grad_kernel<kF32, LANES, E>, norm_grad_kernel<kBF16, LANES, E>}}
+struct NormGradShape {
+    uint32_t cols, rows;
+    void (*kernel[2])(const NormGradArgs);
+};
+
+#define NORM_SHAPE(LANES, E) {LANES * E, kNormThreads<LANES> / LANES, kNormThreads<LANES>, {norm_kernel<kF32, LANES, E>, norm_kernel<kBF16, LANES, E>}}
 static const NormShape kNormShapes[] = {NORM_SHAPE(8, 8), NORM_SHAPE(16, 8), NORM_SHAPE(32, 8), NORM_SHAPE(64, 8), NORM_SHAPE(64, 16),
                                         NORM_SHAPE(256, 8), NORM_SHAPE(256, 16), NORM_SHAPE(512, 16), NORM_SHAPE(1024, 16)};
 #undef NORM_SHAPE
 
-static const NormShape *norm_shape(int64_t cols)
+#define GRAD_SHAPE(LANES, E, KEEP) {LANES * E, kGradThreads / LANES, {norm_grad_kernel<kF32, LANES, E, KEEP>, norm_grad_kernel<kBF16, LANES, E, KEEP>}}
+static const NormGradShape kNormGradShapes[] = {GRAD_SHAPE(8, 8, true), GRAD_SHAPE(16, 8, true), GRAD_SHAPE(32, 8, true), GRAD_SHAPE(64, 8, true), GRAD_SHAPE(128, 8, true),
+                                                GRAD_SHAPE(256, 8, true), GRAD_SHAPE(512, 8, true), GRAD_SHAPE(1024, 8, true), GRAD_SHAPE(1024, 16, false)};
+#undef GRAD_SHAPE
+
+// the narrowest that holds the row, none for rows that no workgroup holds
+template <typename Shape, size_t n>
+static const Shape *shape_for(const Shape (&shapes)[n], int64_t cols)
 {
-    for (const NormShape &s : kNormShapes)
+    for (const Shape &s : shapes)
         if (cols <= s.cols)
             return &s;
     return nullptr;
@@ -652,34 +715,49 @@ static const NormShape *norm_shape(int64_t cols)
 
 static uint32_t at_most(uint64_t v, uint32_t most) { return (uint32_t)(v < most ? v : most); }
 
-static uint32_t pitch_of(int64_t cols) { return (uint32_t)((cols + 3) & ~3ll); }
+static uint32_t pitch_of(int64_t cols) { return (uint32_t)((cols + 7) & ~7ll); }      // whole chunks of either type
 
 static uint32_t norm_strips(int64_t rows, int64_t cols)
 {
-    const NormShape *const s = norm_shape(cols);
+    const NormGradShape *const s = shape_for(kNormGradShapes, cols);
     if (!s)
         return at_most(rows, 64);
-    return at_most((rows + s->grad_rows - 1) / s->grad_rows, 131072 / s->grad_threads);
+    // Two rounds of one workgroup cost less than a second launch (16 rows of 1024 bf16: 5.1 us, with it 7.2; four rounds 7.5 and 7.3).
+    const uint64_t rounds = (rows + s->rows - 1) / s->rows;
+    if (rounds <= 2)
+        return at_most(rounds, 1);
+    if (rounds <= kGradStrips)
+        return (uint32_t)rounds;
+    // as many rounds for each, where that saves a quarter of the strips (and their sums)
+    const uint64_t each = (rounds + kGradStrips - 1) / kGradStrips, even = (rounds + each - 1) / each;
+    return even <= kGradStrips * 3 / 4 ? (uint32_t)even : kGradStrips;
 }
 
-// The tile of GELU's kernels: as many lanes as waste least at the end of a row.
-static void gelu_tile(int64_t rows, int64_t cols, tmask_dtype dt, GeluArgs *p)
+// The tile of GELU's kernels: lanes that waste little at the end of a row, but rather many, since short pieces of rows cut more lines
+// (30000 rows of 1400: bf16 in pieces of 16 lanes 49 us, of 64 lanes 40; fp32 of 32 lanes 82, of 128 lanes 72).
+static void gelu_tile(int64_t rows, int64_t cols, tmask_dtype dt, bool grad, GeluArgs *p)
 {
     const uint32_t n = dt == TMASK_F32 ? 4 : 8;
     p->chunks = (uint32_t)((cols + n - 1) / n);
-    uint32_t best = 0, waste = ~0u;
+    static const uint64_t price[9] = {0, 0, 0, 150, 135, 118, 106, 102, 100};
+    uint32_t best = 8;
+    uint64_t least = ~0ull;
     for (uint32_t l = 8; l >= 3 && (l == 8 || p->chunks < 1u << 20); l--) {
-        const uint32_t lost = ((p->chunks + (1u << l) - 1) >> l << l) - p->chunks;
-        if (lost < waste) {
-            waste = lost;
+        const uint64_t cost = (((uint64_t)p->chunks + (1u << l) - 1) >> l << l) * price[l];
+        if (cost < least) {
+            least = cost;
             best = l;
         }
     }
     p->lanes_log2 = best;
     p->groups = (p->chunks + (1u << best) - 1) >> best;
-    const uint64_t high = kThreads >> best;
-    const uint64_t strips = (rows + high - 1) / high, most = (2048 + p->groups - 1) / p->groups;
-    p->strips = (uint32_t)(strips < most ? strips : most);
+    const uint64_t high = (grad ? kGradThreads : kThreads) >> best;
+    // Gradients: up to 16 elements a thread, a second launch costs more than workgroups beside each other alone (16 rows of 1024 bf16
+    // 5.3 and 7.0 us; 32 elements 8.4 and 7.0).
+    // (Of the gradients' workgroups a compute unit holds one: one more than there are units doubles the time.)
+    const uint64_t rounds = (rows + high - 1) / high, all = grad ? kGradStrips : 2048, most = p->groups < all ? all / p->groups : 1;
+    const uint64_t each = grad && rounds * n <= 16 ? 16 / n : rounds <= most ? 1 : grad ? (rounds + most - 1) / most : 0;
+    p->strips = (uint32_t)(each ? (rounds + each - 1) / each : most);
     p->pitch = pitch_of(cols);
 }
 
@@ -727,7 +805,7 @@ extern "C" int tmask_layer_norm(const tmask_norm_desc *desc, tmask_dtype dt, tma
     NormArgs p{d.x, d.residual, d.weight, d.bias, d.y, d.total, d.mean, d.rstd, (size_t)d.ld_x, (size_t)d.ld_residual,
                (size_t)d.ld_y, (size_t)d.ld_total, (uint32_t)d.rows, (uint32_t)d.cols, param_dt == TMASK_F32, eps, (float)(1.0 / (double)d.cols)};
     hipStream_t stream = (hipStream_t)hip_stream;
-    if (const NormShape *const shape = norm_shape(d.cols))
+    if (const NormShape *const shape = shape_for(kNormShapes, d.cols))
         hipLaunchKernelGGL(shape->kernel[dt], dim3(at_most((d.rows + shape->rows - 1) / shape->rows, 524288 / shape->threads)), dim3(shape->threads), 0,
                            stream, p);
     else
@@ -758,7 +836,7 @@ extern "C" int tmask_layer_norm_backward(const tmask_norm_grad_desc *desc, tmask
     NormGradArgs p{d.dy, d.x, d.weight, d.dtotal, d.mean, d.rstd, d.dx, d.dweight, d.dbias, (float *)workspace, (size_t)d.ld_dy, (size_t)d.ld_x,
                    (size_t)d.ld_dtotal, (size_t)d.ld_dx, (uint32_t)d.rows, (uint32_t)d.cols, param_dt == TMASK_F32, strips, pitch_of(d.cols),
                    (float)(1.0 / (double)d.cols)};
-    const NormShape *const shape = norm_shape(d.cols);
+    const NormGradShape *const shape = shape_for(kNormGradShapes, d.cols);
     if (d.rows > 0) {
         TMASK_TRY(check_rows("dy", d.dy, d.ld_dy, d.rows, d.cols, size, true));
         TMASK_TRY(check_rows("x", d.x, d.ld_x, d.rows, d.cols, size, true));
@@ -770,7 +848,7 @@ extern "C" int tmask_layer_norm_backward(const tmask_norm_grad_desc *desc, tmask
         if (sums)
             TMASK_TRY(check_workspace(workspace, workspace_bytes, tmask_layer_norm_workspace_bytes(d.rows, d.cols)));
         if (shape) {
-            hipLaunchKernelGGL(shape->grad[dt], dim3(strips), dim3(shape->grad_threads), 0, stream, p);
+            hipLaunchKernelGGL(shape->kernel[dt], dim3(strips), dim3(kGradThreads), 0, stream, p);
         } else {
             if (sums)
                 hipLaunchKernelGGL(dt == TMASK_F32 ? norm_long_columns_kernel<kF32> : norm_long_columns_kernel<kBF16>,
@@ -805,7 +883,7 @@ extern "C" int tmask_bias_gelu(const tmask_gelu_desc *desc, tmask_dtype dt, tmas
     TMASK_TRY(check_vector("bias", d.bias, size_of(param_dt), false));
     GeluArgs p{nullptr, d.x, d.bias, d.y, nullptr, nullptr, 0, (size_t)d.ld_x, (size_t)d.ld_y, (uint32_t)d.rows, (uint32_t)d.cols, 0,
                param_dt == TMASK_F32, 0, 0, 0, 0};
-    gelu_tile(d.rows, d.cols, dt, &p);
+    gelu_tile(d.rows, d.cols, dt, false, &p);
     static void (*const kernels[2][2])(const GeluArgs) = {GELU_KERNELS(kF32, false), GELU_KERNELS(kBF16, false)};
     hipLaunchKernelGGL(kernels[dt][form], dim3(p.groups * p.strips), dim3(kThreads), 0, (hipStream_t)hip_stream, p);
     return launched("GELU launch");
@@ -818,7 +896,7 @@ extern "C" size_t tmask_bias_gelu_workspace_bytes(int64_t rows, int64_t cols)
     size_t strips = 0;
     for (const tmask_dtype dt : {TMASK_F32, TMASK_BF16}) {
         GeluArgs p;
-        gelu_tile(rows, cols, dt, &p);
+        gelu_tile(rows, cols, dt, true, &p);
         strips = p.strips > strips ? p.strips : strips;
     }
     return strips * pitch_of(cols) * 4u;
@@ -838,7 +916,7 @@ extern "C" int tmask_bias_gelu_backward(const tmask_gelu_grad_desc *desc, tmask_
     hipStream_t stream = (hipStream_t)hip_stream;
     GeluArgs p{d.dy, d.x, d.bias, d.dx, d.dbias, (float *)workspace, (size_t)d.ld_dy, (size_t)d.ld_x, (size_t)d.ld_dx, (uint32_t)d.rows,
                (uint32_t)d.cols, 0, param_dt == TMASK_F32, 0, 0, 0, 0};
-    gelu_tile(d.rows, d.cols, dt, &p);
+    gelu_tile(d.rows, d.cols, dt, true, &p);
     if (d.rows > 0) {
         TMASK_TRY(check_rows("dy", d.dy, d.ld_dy, d.rows, d.cols, size_of(dt), true));
         TMASK_TRY(check_rows("x", d.x, d.ld_x, d.rows, d.cols, size_of(dt), true));
@@ -847,7 +925,7 @@ extern "C" int tmask_bias_gelu_backward(const tmask_gelu_grad_desc *desc, tmask_
         if (d.dbias)
             TMASK_TRY(check_workspace(workspace, workspace_bytes, tmask_bias_gelu_workspace_bytes(d.rows, d.cols)));
         static void (*const kernels[2][2])(const GeluArgs) = {GELU_KERNELS(kF32, true), GELU_KERNELS(kBF16, true)};
-        hipLaunchKernelGGL(kernels[dt][form], dim3(p.groups * p.strips), dim3(kThreads), 0, stream, p);
+        hipLaunchKernelGGL(kernels[dt][form], dim3(p.groups * p.strips), dim3(kGradThreads), 0, stream, p);
     }
     if (d.dbias && p.strips != 1)
         sum_columns(p.partial, d.dbias, nullptr, d.cols, p.strips, 1, param_dt, stream);
