@@ -137,15 +137,15 @@ __device__ __forceinline__ float row_sum(float v, float *red)
 {
     v = lanes_reduce<Sum, LANES < 64 ? LANES : 64>(v);
     if constexpr (LANES > 64) {
-        constexpr int W = T / 64;
-        static_assert(LANES == T, "a row has the whole workgroup");
+        constexpr uint32_t kWaves = LANES / 64;                                 // of a row
+        const uint32_t first = threadIdx.x / LANES * kWaves;
         if ((threadIdx.x & 63) == 0)
             red[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = red[0];
+        v = red[first];
 #pragma unroll
-        for (int w = 1; w < W; w++)
-            v += red[w];
+        for (uint32_t w = 1; w < kWaves; w++)
+            v += red[first + w];
     }
     return v;
 }
@@ -156,12 +156,31 @@ __global__ void __launch_bounds__(kNormThreads<LANES>) norm_kernel(const NormArg
     constexpr int T = kNormThreads<LANES>, N = kElems<DT>, C = E / N, kRows = T / LANES;
     __shared__ float red[2][LANES > 64 ? T / 64 : 1];
     const uint32_t lane = threadIdx.x % LANES;
-    float w[E], b[E];
     uint32_t left[C];
 #pragma unroll
     for (int i = 0; i < C; i++) {
         const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
         left[i] = c >= p.cols ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
+    }
+    u32x4 raw[C], more[C];
+    auto fetch = [&](uint32_t r) {
+#pragma unroll
+        for (int i = 0; i < C; i++) {
+            const size_t c = (lane + (uint32_t)(i * LANES)) * N;
+            raw[i] = more[i] = u32x4{0u, 0u, 0u, 0u};
+            if (left[i] && r < p.rows) {
+                raw[i] = fetch_chunk<DT>(p.x, r * p.ld_x + c, left[i], p.cols);
+                if (p.residual)
+                    more[i] = fetch_chunk<DT>(p.residual, r * p.ld_residual + c, left[i], p.cols);
+            }
+        }
+    };
+    const uint32_t first = blockIdx.x * kRows + threadIdx.x / LANES, step = gridDim.x * kRows;
+    fetch(first);                                                               // on the way while the parameters are read
+    float w[E], b[E];
+#pragma unroll
+    for (int i = 0; i < C; i++) {
+        const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
         float v[N];
 #pragma unroll
         for (int e = 0; e < N; e++)
@@ -180,31 +199,22 @@ __global__ void __launch_bounds__(kNormThreads<LANES>) norm_kernel(const NormArg
             b[i * N + e] = v[e];
     }
     const bool whole = p.cols == (uint32_t)(LANES * E);
-    for (uint32_t r = blockIdx.x * kRows + threadIdx.x / LANES; r < p.rows; r += gridDim.x * kRows) {
-        u32x4 raw[C], more[C];
-#pragma unroll
-        for (int i = 0; i < C; i++) {
-            const size_t c = (lane + (uint32_t)(i * LANES)) * N;
-            raw[i] = more[i] = u32x4{0u, 0u, 0u, 0u};
-            if (left[i]) {
-                raw[i] = load_chunk<DT>(p.x, r * p.ld_x + c, left[i]);
-                if (p.residual)
-                    more[i] = load_chunk<DT>(p.residual, r * p.ld_residual + c, left[i]);
-            }
-        }
+    uint32_t r = first;
+    for (uint32_t r0 = blockIdx.x * kRows; r0 < p.rows; r0 += step, r += step) {  // the same number of rounds for all: barriers are inside
+        const bool exists = r < p.rows;
         float t[E], s = 0.f;
 #pragma unroll
         for (int i = 0; i < C; i++) {
             float v[N], u[N];
-            unpack<DT>(raw[i], v);
-            unpack<DT>(more[i], u);
+            unpack<DT>(settle<DT>(raw[i], left[i], p.cols), v);
+            unpack<DT>(settle<DT>(more[i], left[i], p.cols), u);
 #pragma unroll
             for (int e = 0; e < N; e++) {
                 v[e] += u[e];
                 t[i * N + e] = v[e];
                 s += v[e];
             }
-            if (p.total && left[i])
+            if (p.total && left[i] && exists)
                 store_chunk<DT>(p.total, r * p.ld_total + (size_t)(lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
         }
         const float mean = row_sum<LANES, T>(s, red[0]) * p.per_col;
@@ -224,13 +234,14 @@ __global__ void __launch_bounds__(kNormThreads<LANES>) norm_kernel(const NormArg
 #pragma unroll
             for (int e = 0; e < N; e++)
                 v[e] = t[i * N + e] * rstd * w[i * N + e] + b[i * N + e];
-            if (left[i])
+            if (left[i] && exists)
                 store_chunk<DT>(p.y, r * p.ld_y + (size_t)(lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
         }
-        if (p.mean && lane == 0) {
+        if (p.mean && lane == 0 && exists) {
             p.mean[r] = mean;
             p.rstd[r] = rstd;
         }
+        fetch(r + step);
     }
 }
 
@@ -328,24 +339,11 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
     constexpr int kShared = LANES < 64 ? W : kRows;                             // sets of column sums that the workgroup adds up
     __shared__ float red[2][2 * W];
     const uint32_t lane = threadIdx.x % LANES;
-    float w[C][N], dw[C][N], db[C][N];
     uint32_t left[C];
-    auto weights = [&](int i, float (&v)[N]) {
-#pragma unroll
-        for (int e = 0; e < N; e++)
-            v[e] = 1.f;
-        if (p.weight && left[i])
-            load_params<N>(p.weight, p.param_f32, (lane + (uint32_t)(i * LANES)) * N, left[i], v);
-    };
 #pragma unroll
     for (int i = 0; i < C; i++) {
         const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
         left[i] = c >= p.cols ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
-        if constexpr (KEEP)
-            weights(i, w[i]);
-#pragma unroll
-        for (int e = 0; e < N; e++)
-            dw[i][e] = db[i][e] = 0.f;
     }
     struct Row {
         u32x4 dy[C], x[C], more[C];
@@ -357,20 +355,36 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
             const size_t c = (lane + (uint32_t)(i * LANES)) * N;
             row.dy[i] = row.x[i] = row.more[i] = u32x4{0u, 0u, 0u, 0u};
             if (left[i] && r < p.rows) {
-                row.dy[i] = load_chunk<DT>(p.dy, r * p.ld_dy + c, left[i]);
-                row.x[i] = load_chunk<DT>(p.x, r * p.ld_x + c, left[i]);
+                row.dy[i] = fetch_chunk<DT>(p.dy, r * p.ld_dy + c, left[i], p.cols);
+                row.x[i] = fetch_chunk<DT>(p.x, r * p.ld_x + c, left[i], p.cols);
                 if (p.dtotal)
-                    row.more[i] = load_chunk<DT>(p.dtotal, r * p.ld_dtotal + c, left[i]);
+                    row.more[i] = fetch_chunk<DT>(p.dtotal, r * p.ld_dtotal + c, left[i], p.cols);
             }
         }
         row.mean = r < p.rows ? p.mean[r] : 0.f;
         row.rstd = r < p.rows ? p.rstd[r] : 0.f;
     };
-    // the same number of rounds for the whole workgroup: barriers are inside
     const uint32_t step = p.strips * kRows;
     uint32_t r = blockIdx.x * kRows + threadIdx.x / LANES, turn = 0;
     if constexpr (KEEP)
         fetch(r, next);
+    float w[C][N], dw[C][N], db[C][N];
+    auto weights = [&](int i, float (&v)[N]) {
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            v[e] = 1.f;
+        if (p.weight && left[i])
+            load_params<N>(p.weight, p.param_f32, (lane + (uint32_t)(i * LANES)) * N, left[i], v);
+    };
+#pragma unroll
+    for (int i = 0; i < C; i++) {
+        if constexpr (KEEP)
+            weights(i, w[i]);
+#pragma unroll
+        for (int e = 0; e < N; e++)
+            dw[i][e] = db[i][e] = 0.f;
+    }
+    // the same number of rounds for the whole workgroup: barriers are inside
     for (uint32_t r0 = blockIdx.x * kRows; r0 < p.rows; r0 += step, r += step, turn ^= 1) {
         if constexpr (!KEEP)
             fetch(r, next);
@@ -383,8 +397,8 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
 #pragma unroll
         for (int i = 0; i < C; i++) {
             float v[N], u[N];
-            unpack<DT>(row.dy[i], v);
-            unpack<DT>(row.x[i], u);
+            unpack<DT>(settle<DT>(row.dy[i], left[i], p.cols), v);
+            unpack<DT>(settle<DT>(row.x[i], left[i], p.cols), u);
             if constexpr (!KEEP)
                 weights(i, w[i]);
 #pragma unroll
@@ -422,7 +436,7 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
 #pragma unroll
         for (int i = 0; i < C; i++) {
             float v[N];
-            unpack<DT>(row.more[i], v);
+            unpack<DT>(settle<DT>(row.more[i], left[i], p.cols), v);
 #pragma unroll
             for (int e = 0; e < N; e++)
                 v[e] += row.rstd * (d[i * N + e] - s1 - h[i * N + e] * s2);
@@ -593,33 +607,36 @@ __global__ void __launch_bounds__(kGeluThreads<GRAD>) gelu_kernel(const GeluArgs
     const uint32_t group = blockIdx.x % p.groups, strip = blockIdx.x / p.groups;
     const uint32_t chunk = group * lanes + (threadIdx.x & (lanes - 1u)), y = threadIdx.x >> p.lanes_log2;
     const uint32_t c = chunk * N, left = chunk >= p.chunks ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
+    const uint32_t step = p.strips * high;
+    u32x4 x[kGeluRows], d[kGeluRows];
+    auto fetch = [&](uint64_t r0) {
+#pragma unroll
+        for (int i = 0; i < kGeluRows; i++) {
+            const uint64_t r = r0 + (uint64_t)i * step;
+            x[i] = d[i] = u32x4{0u, 0u, 0u, 0u};
+            if (left && r < p.rows) {
+                x[i] = fetch_chunk<DT>(p.x, r * p.ld_x + c, left, p.cols);
+                if constexpr (GRAD)
+                    d[i] = fetch_chunk<DT>(p.dy, r * p.ld_dy + c, left, p.cols);
+            }
+        }
+    };
+    fetch(strip * high + y);                                                    // on the way while the bias is read
     float b[N], sum[N];
 #pragma unroll
     for (int e = 0; e < N; e++)
         b[e] = sum[e] = 0.f;
     if (p.bias && left)
         load_params<N>(p.bias, p.param_f32, c, left, b);
-    const uint32_t step = p.strips * high;
     if (left)
-        for (uint64_t r0 = strip * high + y; r0 < p.rows; r0 += (uint64_t)kGeluRows * step) {
-            u32x4 x[kGeluRows], d[kGeluRows];
-#pragma unroll
-            for (int i = 0; i < kGeluRows; i++) {
-                const uint64_t r = r0 + (uint64_t)i * step;
-                x[i] = d[i] = u32x4{0u, 0u, 0u, 0u};
-                if (r < p.rows) {
-                    x[i] = load_chunk<DT>(p.x, r * p.ld_x + c, left);
-                    if constexpr (GRAD)
-                        d[i] = load_chunk<DT>(p.dy, r * p.ld_dy + c, left);
-                }
-            }
+        for (uint64_t r0 = strip * high + y; r0 < p.rows;) {
 #pragma unroll
             for (int i = 0; i < kGeluRows; i++) {
                 const uint64_t r = r0 + (uint64_t)i * step;
                 if (r < p.rows) {
                     float v[N], u[N];
-                    unpack<DT>(x[i], v);
-                    unpack<DT>(d[i], u);
+                    unpack<DT>(settle<DT>(x[i], left, p.cols), v);
+                    unpack<DT>(settle<DT>(d[i], left, p.cols), u);
 #pragma unroll
                     for (int e = 0; e < N; e++) {
                         v[e] = gelu<FORM, GRAD>(v[e] + b[e]);
@@ -631,6 +648,9 @@ __global__ void __launch_bounds__(kGeluThreads<GRAD>) gelu_kernel(const GeluArgs
                     store_chunk<DT>(p.out, r * p.ld_out + c, left, pack<DT>(v));
                 }
             }
+            r0 += (uint64_t)kGeluRows * step;
+            if (r0 < p.rows)
+                fetch(r0);
         }
     if constexpr (GRAD) {
         if (!p.dbias)

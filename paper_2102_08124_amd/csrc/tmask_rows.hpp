@@ -77,6 +77,34 @@ __device__ __forceinline__ u32x4 load_chunk(const void *p, size_t i, uint32_t le
     return v;
 }
 
+// The same for a row of `cols` elements, in two steps: the load, a single one if the row has a chunk's elements at all (the one at
+// the row's end, which ends with what is wanted), and what moves the wanted elements to the front and leaves 0 behind them.  Where a row of
+// a wavefront's lanes fetches element by element and composes, everything that is in flight waits for it (the gradients of a layer norm of 13731
+// rows of 4476 bf16 took 175 us that way, of 4480 93).
+template <int DT>
+__device__ __forceinline__ u32x4 fetch_chunk(const void *p, size_t i, uint32_t left, uint32_t cols)
+{
+    constexpr uint32_t N = kElems<DT>;
+    return load_chunk<DT>(p, left < N && cols >= N ? i - (N - left) : i, cols >= N ? N : left);
+}
+
+template <int DT>
+__device__ __forceinline__ u32x4 settle(u32x4 raw, uint32_t left, uint32_t cols)
+{
+    constexpr uint32_t N = kElems<DT>;
+    if (cols % N && cols > N && left < N) {                                     // the first two are the same for all
+        const uint32_t s = N - left;
+        if constexpr (DT == kBF16)
+            if (s & 1u)
+                raw = u32x4{raw.x >> 16 | raw.y << 16, raw.y >> 16 | raw.z << 16, raw.z >> 16 | raw.w << 16, raw.w >> 16};
+        if (s & N / 4)
+            raw = u32x4{raw.y, raw.z, raw.w, 0u};
+        if (s & N / 2)
+            raw = u32x4{raw.z, raw.w, 0u, 0u};
+    }
+    return raw;
+}
+
 // A whole chunk at `offset` bytes from an address that is the same for the wavefront, which then is held in scalar registers.
 // STREAM: with the non-temporal hint, for what is read or written once and does not fit the caches.
 template <int DT, bool STREAM = false>
