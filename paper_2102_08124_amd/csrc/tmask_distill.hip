@@ -261,6 +261,48 @@ __device__ __forceinline__ u32x4 pull(const DistillArgs &a, u32x4 raw, float z_m
     return pack<DT>(v);
 }
 
+// Turns the logits of a thread's entries into probabilities (part of the teacher's sum, which is 1 / part and whose logarithm is t_log); the
+// result is what they add to the loss, without T^2.
+template <uint32_t T>
+__device__ __forceinline__ float take_entries(const DistillArgs &a, const List &list, float t_max, float t_sum, float z_max, float z_sum)
+{
+    const float t_log = logf(t_sum), z_log = logf(z_sum), part = 1.f / t_sum;
+    float loss = 0.f;
+    for (uint32_t j = threadIdx.x; j < a.k; j += T)
+        if (list.at[j] >= 0) {
+            const float t = list.t[j] - t_max, p = exp_of(a, t) * part;
+            const float log_q = (list.z[j] - z_max) * a.per_t - z_log;
+            loss += log_q == -INFINITY ? INFINITY : p * ((t * a.per_t - t_log) - log_q);
+            list.t[j] = p;
+        }
+    return loss;
+}
+
+template <uint32_t T>
+__device__ __forceinline__ float entries_sum(const DistillArgs &a, const List &list, float t_max)
+{
+    float sum = 0.f;
+    for (uint32_t j = threadIdx.x; j < a.k; j += T)
+        if (list.at[j] >= 0)
+            sum += exp_of(a, list.t[j] - t_max);
+    return sum;
+}
+
+// The row's results, by thread 0, from the wavefronts' parts of the loss.
+template <int W>
+__device__ __forceinline__ void write_row(const DistillArgs &a, uint32_t r, const float *parts, bool some, float z_max, float z_sum)
+{
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; w++)
+        sum += parts[w];
+    a.loss[r] = some ? a.temperature * a.temperature * sum : 0.f;
+    if (a.row_max) {
+        a.row_max[r] = z_max;
+        a.row_sum[r] = z_sum;
+    }
+}
+
 // ---------------------------------------------------------------------------------------------------------------------
 // A row in the registers of one workgroup: T threads with P chunks each.  The logits are read once, added up as they arrive, and the
 // gradient is taken from the registers.
@@ -304,23 +346,11 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
                 add_chunks<DT, G>(a, run, raw[i]);
         float z_max = run.max;
         group_reduce<Max, Max, W>(t_max, z_max, red);
-        float t_sum = 0.f, z_sum = relative(a, run, z_max);
-        for (uint32_t j = threadIdx.x; j < a.k; j += T)
-            if (list.at[j] >= 0)
-                t_sum += exp_of(a, list.t[j] - t_max);
+        float t_sum = entries_sum<T>(a, list, t_max), z_sum = relative(a, run, z_max);
         group_reduce<Sum, Sum, W>(t_sum, z_sum, red + 2 * W);
 
         const bool some = t_max != -INFINITY;
-        const float t_log = logf(t_sum), z_log = logf(z_sum), t_part = 1.f / t_sum;
-        float loss = 0.f;
-        for (uint32_t j = threadIdx.x; j < a.k; j += T)
-            if (list.at[j] >= 0) {
-                const float t = list.t[j] - t_max, p = exp_of(a, t) * t_part;
-                const float log_q = (list.z[j] - z_max) * a.per_t - z_log;
-                loss += log_q == -INFINITY ? INFINITY : p * ((t * a.per_t - t_log) - log_q);
-                list.t[j] = p;
-            }
-        loss = lanes_reduce<Sum, 64>(loss);
+        const float loss = lanes_reduce<Sum, 64>(take_entries<T>(a, list, t_max, t_sum, z_max, z_sum));
         if ((threadIdx.x & 63) == 0)
             red[4 * W + (threadIdx.x >> 6)] = loss;
 
@@ -340,17 +370,8 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
                 store_one<DT>(a.dlogits, d0 + edge.at, none ? 0.f : exp_of(a, single - z_max) * g_q);
         }
         __syncthreads();
-        if (threadIdx.x == 0) {
-            float sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < W; w++)
-                sum += red[4 * W + w];
-            a.loss[r] = some ? a.temperature * a.temperature * sum : 0.f;
-            if (a.row_max) {
-                a.row_max[r] = z_max;
-                a.row_sum[r] = z_sum;
-            }
-        }
+        if (threadIdx.x == 0)
+            write_row<W>(a, r, red + 4 * W, some, z_max, z_sum);
         if (a.dlogits && !none) {
             const bool repeats = *list.repeats != 0;
             for (uint32_t j = threadIdx.x; j < a.k; j += T) {
@@ -443,6 +464,42 @@ __global__ void __launch_bounds__(kSlice) distill_part_kernel(const DistillArgs 
     }
 }
 
+// The loss alone of rows that are added up without being held, so that a compute unit has eight workgroups' loads in flight.
+template <int DT>
+__global__ void __launch_bounds__(kSlice) distill_loss_kernel(const DistillArgs a)
+{
+    constexpr int W = kSlice / 64;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    float *const red = (float *)lds;
+    const List list = list_in(red + 5 * W, a);
+    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const Part p = part_of<DT>(a, r);                                       // the whole row
+        const size_t z0 = r * a.ld_logits;
+        const uint32_t edge_bits = p.edge.there ? load_bits<DT>(a.logits, z0 + p.edge.at) : 0u;
+        float t_max = a.k ? read_list<kSlice>(a, r, list, [&](int32_t at, uint32_t) { return load_bits<DT>(a.logits, z0 + (uint32_t)at); },
+                                                 from_bits<DT>, [](int32_t) { return false; })
+                             : -INFINITY;
+        Running run = start(a, p.edge, from_bits<DT>(edge_bits));
+        for (uint32_t c0 = p.begin; c0 < p.end; c0 += kAhead * kSlice) {
+            u32x4 raw[kAhead];
+            fetch<DT, true>(a, p, c0, raw);
+            add_chunks<DT, kAhead>(a, run, raw);
+        }
+        float z_max = run.max;
+        group_reduce<Max, Max, W>(t_max, z_max, red);
+        float t_sum = entries_sum<kSlice>(a, list, t_max), z_sum = relative(a, run, z_max);
+        group_reduce<Sum, Sum, W>(t_sum, z_sum, red + 2 * W);
+        const float loss = lanes_reduce<Sum, 64>(take_entries<kSlice>(a, list, t_max, t_sum, z_max, z_sum));
+        if ((threadIdx.x & 63) == 0)
+            red[4 * W + (threadIdx.x >> 6)] = loss;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            write_row<W>(a, r, red + 4 * W, t_max != -INFINITY, z_max, z_sum);
+        if (r + gridDim.x < a.rows)
+            __syncthreads();
+    }
+}
+
 // JOIN: after distill_part_kernel, with the loss; otherwise the gradient from the row's statistics.
 template <int DT, bool JOIN>
 __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs a)
@@ -492,39 +549,15 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
                                       [&](int32_t at) { return a.dlogits && in_part(p, at); });
         }
         group_reduce<Max, Max, W>(t_max, unused, red);
-        for (uint32_t j = threadIdx.x; j < a.k; j += kSlice)
-            if (list.at[j] >= 0)
-                t_sum += exp_of(a, list.t[j] - t_max);
+        t_sum = entries_sum<kSlice>(a, list, t_max);
         group_reduce<Sum, Sum, W>(t_sum, unused, red + 2 * W);
         const bool some = t_max != -INFINITY;
-        const float t_log = logf(t_sum), z_log = logf(z_sum), t_part = 1.f / t_sum;
-        float loss = 0.f;
-        for (uint32_t j = threadIdx.x; j < a.k; j += kSlice)
-            if (list.at[j] >= 0) {
-                const float t = list.t[j] - t_max, q = exp_of(a, t) * t_part;
-                if (JOIN && p.part == 0) {
-                    const float log_q = (list.z[j] - z_max) * a.per_t - z_log;
-                    loss += log_q == -INFINITY ? INFINITY : q * ((t * a.per_t - t_log) - log_q);
-                }
-                list.t[j] = q;
-            }
-        if (JOIN && p.part == 0) {
-            loss = lanes_reduce<Sum, 64>(loss);
-            if ((threadIdx.x & 63) == 0)
-                red[4 * W + (threadIdx.x >> 6)] = loss;
-        }
+        const float loss = lanes_reduce<Sum, 64>(take_entries<kSlice>(a, list, t_max, t_sum, z_max, z_sum));
+        if ((threadIdx.x & 63) == 0)
+            red[4 * W + (threadIdx.x >> 6)] = loss;
         __syncthreads();
-        if (JOIN && p.part == 0 && threadIdx.x == 0) {
-            float sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < W; w++)
-                sum += red[4 * W + w];
-            a.loss[p.r] = some ? a.temperature * a.temperature * sum : 0.f;
-            if (a.row_max) {
-                a.row_max[p.r] = z_max;
-                a.row_sum[p.r] = z_sum;
-            }
-        }
+        if (JOIN && p.part == 0 && threadIdx.x == 0)
+            write_row<W>(a, p.r, red + 4 * W, some, z_max, z_sum);
         if (a.dlogits) {
             const float g_q = g / z_sum;
             const bool none = !some || g == 0.f;
@@ -572,6 +605,8 @@ static const RowKernel kManyRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(64, 8), ROW_
                                       ROW_KERNEL(512, 32), ROW_KERNEL(512, 48)};
 static const RowKernel kFewRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(256, 4), ROW_KERNEL(1024, 4), ROW_KERNEL(1024, 8), ROW_KERNEL(512, 32), ROW_KERNEL(512, 48)};
 constexpr int64_t kFew = 256;
+// Without a gradient longer rows need not be held (3000 rows of 64000 fp32: 148 us held, 117 not; of 4000, 1000 chunks, 14.7 both).
+constexpr uint32_t kLossHeld = 1024;
 #undef ROW_KERNEL
 constexpr uint32_t kHeld = 512 * 48;
 
@@ -596,12 +631,12 @@ static Cut cut_rows(int64_t rows, uint32_t chunks, uint32_t least, uint32_t most
 
 static uint32_t chunks_of(int64_t vocab, tmask_dtype dt) { return (uint32_t)(vocab / (dt == TMASK_F32 ? 4 : 8)); }   // of a row at most
 
-static Cut cut_loss(int64_t rows, int64_t vocab, tmask_dtype dt)
+static Cut cut_loss(int64_t rows, int64_t vocab, tmask_dtype dt, bool alone)
 {
     const uint32_t chunks = chunks_of(vocab, dt);
     // A second launch costs 3 us; a row in one workgroup longer, the longer it is and the fewer compute units have one (us, row / parts:
     // 16 rows of 32000 bf16 8.4 / 10.0, of 64000 11.9 / 10.1; 64 rows of 64000 12.6 / 15.4, of 131072 22.8 / 16.5; 256 rows of 131072 34 both).
-    if (chunks <= 4096 || rows >= (chunks <= 8192 ? 64 : chunks <= kHeld ? kFew : INT64_MAX))
+    if (chunks <= 4096 || rows >= (chunks <= 8192 ? 64 : chunks <= kHeld || alone ? kFew + 1 : INT64_MAX))
         return {0, 0};
     return cut_rows(rows, chunks, 512, kAhead * kSlice);
 }
@@ -654,7 +689,7 @@ extern "C" size_t tmask_distill_workspace_bytes(int64_t rows, int64_t vocab)
         return 0;
     size_t most = 0;
     for (const tmask_dtype dt : {TMASK_F32, TMASK_BF16}) {
-        const size_t parts = cut_loss(rows, vocab, dt).parts;
+        const size_t parts = cut_loss(rows, vocab, dt, false).parts;
         const size_t need = parts ? (size_t)rows * (2u * parts + kMaxEntries) * 4u : 0;
         most = need > most ? need : most;
     }
@@ -672,10 +707,15 @@ extern "C" int tmask_distill(const tmask_distill_desc *desc, tmask_dtype dt, tma
     TMASK_TRY(check_vector("row_max", desc->row_max, 4, desc->row_sum != nullptr));
     TMASK_TRY(check_vector("row_sum", desc->row_sum, 4, desc->row_max != nullptr));
     hipStream_t stream = (hipStream_t)hip_stream;
-    const Cut cut = cut_loss(desc->rows, desc->vocab, dt);
+    const Cut cut = cut_loss(desc->rows, desc->vocab, dt, !a.dlogits);
     const size_t list = list_bytes(a.k, a.hash_shift);
     const bool bf16 = dt == TMASK_BF16;
-    if (cut.parts == 0) {
+    if (cut.parts == 0 && !a.dlogits && desc->rows > kFew && chunks_of(desc->vocab, dt) > kLossHeld) {
+        a.parts = 1;
+        a.part_chunks = chunks_of(desc->vocab, dt);
+        hipLaunchKernelGGL(bf16 ? distill_loss_kernel<kBF16> : distill_loss_kernel<kF32>, dim3(grid_of(a.rows)), dim3(kSlice), 20 * (kSlice / 64) + list,
+                           stream, a);
+    } else if (cut.parts == 0) {
         const RowKernel *k = desc->rows <= kFew ? kFewRows : kManyRows;
         while (k->chunks < chunks_of(desc->vocab, dt))
             k++;
