@@ -563,3 +563,63 @@ def test_calls_in_a_graph(rows, cols):
         call()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, outs)), k
+
+
+def _outcome(f):
+    try:
+        f()
+        torch.cuda.synchronize()
+        return None
+    except Exception as e:
+        return type(e), str(e)
+
+
+def test_both_halves_of_the_binding_do_the_same(monkeypatch):
+    """The native half takes the usual arguments and leaves the others to the Python half, which raises what is to be raised."""
+    tm.load_library()
+    m = Maker(15)
+    bf, f32 = torch.bfloat16, torch.float32
+    x, r = m.normal((6, 320), bf), m.normal((6, 320), bf)
+    w, b = m.normal((320,), f32), m.normal((320,), f32)
+    teacher, index = lists(m, 6, 320, 8, bf, 64)
+    o = lambda *s, dt=f32: torch.zeros(s, dtype=dt, device="cuda")          # noqa: E731
+    y, t, mu, rs, dx, dw, db = o(6, 320, dt=bf), o(6, 320, dt=bf), o(6), o(6), o(6, 320, dt=bf), o(320), o(320)
+    loss, dz = o(6), o(6, 320, dt=bf)
+    ws, side = tm.alloc_layer_norm_workspace(x), torch.cuda.Stream()
+    wide = torch.zeros((6, 400), dtype=bf, device="cuda")[:, :320]
+    top, total = x.float().amax(1), (x.float() - x.float().amax(1)[:, None]).exp().sum(1)
+    norm = lambda **k: tm.tmask_layer_norm(**{**dict(x=x, y=y, weight=w, bias=b, residual=r, total=t, mean=mu, rstd=rs), **k})          # noqa: E731
+    back = lambda **k: tm.tmask_layer_norm_backward(**{**dict(dy=r, x=x, mean=top, rstd=total, dx=dx, weight=w, dweight=dw, dbias=db, workspace=ws), **k})   # noqa: E731
+    gelu = lambda **k: tm.tmask_bias_gelu(**{**dict(x=x, y=y, bias=b), **k})          # noqa: E731
+    gback = lambda **k: tm.tmask_bias_gelu_backward(**{**dict(dy=r, x=x, dx=dx, bias=b, dbias=db, workspace=tm.alloc_bias_gelu_workspace(x)), **k})          # noqa: E731
+    dist = lambda **k: tm.tmask_distill(**{**dict(logits=x, teacher=teacher, index=index, temperature=2.0, loss=loss, row_max=mu, row_sum=rs, dlogits=dz, workspace=ws), **k})   # noqa: E731
+    dback = lambda **k: tm.tmask_distill_backward(**{**dict(logits=x, teacher=teacher, index=index, temperature=1.0, row_max=top, row_sum=total, dlogits=dz), **k})          # noqa: E731
+    calls = [norm, back, gelu, gback, dist, dback]
+    cases = [(c, {}) for c in calls] + [(c, dict(stream=side)) for c in calls]
+    cases += [(norm, k) for k in (dict(x=wide), dict(weight=None, bias=None), dict(weight=w.to(bf)), dict(weight=w.to(bf), bias=b.to(bf)), dict(mean=None),
+                                  dict(residual=None), dict(residual=None, total=None), dict(y=y[:, :100]), dict(y=y.float()), dict(x=x.cpu()), dict(x=x[0]),
+                                  dict(x=x[:, ::2]), dict(bias=b[:100]), dict(bias=b.half()), dict(mean=mu.double()), dict(eps=-1.0), dict(eps=1), dict(stream=7),
+                                  dict(x=x.half()), dict(x=torch.nn.Parameter(x)), dict(residual=r.cpu()), dict(rstd=rs[::2]))]
+    cases += [(back, k) for k in (dict(workspace=None), dict(workspace=ws[:64]), dict(workspace=ws.cpu()), dict(dweight=None, dbias=None, workspace=None),
+                                  dict(dtotal=y), dict(dtotal=y[:3]), dict(dweight=dw.to(bf)), dict(mean=None), dict(dy=r.float()))]
+    cases += [(gelu, k) for k in (dict(tanh=True), dict(tanh=1), dict(bias=None), dict(y=x[:4]), dict(bias=w[:7]))]
+    cases += [(gback, k) for k in (dict(tanh=True), dict(dbias=None, workspace=None), dict(workspace=None), dict(dy=None), dict(dbias=db.to(bf)))]
+    cases += [(dist, k) for k in (dict(dlogits=None), dict(temperature=0.0), dict(temperature=2), dict(index=index.int()), dict(index=index.short()), dict(index=index[:, :4]),
+                                  dict(teacher=teacher.float()), dict(teacher=teacher[0]), dict(loss=None), dict(loss=loss[:3]), dict(row_weight=mu.double()), dict(row_max=None),
+                                  dict(dlogits=dz.float()), dict(teacher=teacher[:, :0], index=index[:, :0]), dict(teacher=teacher.cpu()), dict(logits=x.half()))]
+    cases += [(dback, k) for k in (dict(row_max=None), dict(dlogits=None), dict(index=index.int()), dict(logits=x[:, ::2]), dict(row_weight=top))]
+    kept, seen = [y, t, mu, rs, dx, dw, db, loss, dz], set()
+    native = tm._calls
+    assert native is not tm._ThroughCtypes
+    for k, (call, args) in enumerate(cases):
+        got = []
+        for half in (native, tm._ThroughCtypes):
+            monkeypatch.setattr(tm, "_calls", half)
+            for v in kept:
+                v.zero_()
+            torch.cuda.synchronize()
+            got.append((_outcome(lambda: call(**args)), [v.clone() for v in kept]))
+        assert got[0][0] == got[1][0], (k, args, got[0][0], got[1][0])
+        assert all(torch.equal(p, q) for p, q in zip(got[0][1], got[1][1])), (k, args)
+        seen.add(None if got[0][0] is None else got[0][0][0])
+    assert {None, tm.TmaskError, TypeError, ValueError} <= seen
