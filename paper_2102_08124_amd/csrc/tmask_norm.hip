@@ -682,21 +682,35 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(const ColumnArgs p)
     __shared__ float sums[32][33];
     const uint32_t x = threadIdx.x % 8u, y = threadIdx.x / 8u, c = blockIdx.x * 32u + x * 4u;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    if (c < p.cols)                                                             // the pitch is a multiple of eight
-#pragma unroll 4
-        for (uint32_t k = y; k < p.strips; k += 32u)
-            s += *(const f32x4 *)(p.partial + ((size_t)k * p.sums + blockIdx.y) * p.pitch + c);
+    if (c < p.cols && p.strips) {                                               // the pitch is a multiple of eight
+        const float *const from = p.partial + (size_t)blockIdx.y * p.pitch + c;
+        const size_t row = (size_t)p.sums * p.pitch;
+        constexpr int kAll = kGradStrips / 32;                                  // all in flight together
+        f32x4 v[kAll];
+#pragma unroll
+        for (int i = 0; i < kAll; i++) {
+            const uint32_t k = y + (uint32_t)i * 32u;
+            v[i] = *(const f32x4 *)(from + (k < p.strips ? k : 0u) * row);
+        }
+#pragma unroll
+        for (int i = 0; i < kAll; i++)
+            if (y + (uint32_t)i * 32u < p.strips)
+                s += v[i];
+        for (uint32_t k = kGradStrips + y; k < p.strips; k += 32u)
+            s += *(const f32x4 *)(from + k * row);
+    }
 #pragma unroll
     for (int e = 0; e < 4; e++)
         sums[y][x * 4 + e] = s[e];
     __syncthreads();
-    if (threadIdx.x < 32u && blockIdx.x * 32u + threadIdx.x < p.cols) {
-        float t = 0.f;
+    // 8 lanes a column
+    float t = 0.f;
 #pragma unroll
-        for (int k = 0; k < 32; k++)
-            t += sums[k][threadIdx.x];
-        store_param(out, p.param_f32, blockIdx.x * 32u + threadIdx.x, t);
-    }
+    for (uint32_t k = 0; k < 4; k++)
+        t += sums[x * 4 + k][y];
+    t = lanes_reduce<Sum, 8>(t);
+    if (x == 0 && blockIdx.x * 32u + y < p.cols)
+        store_param(out, p.param_f32, blockIdx.x * 32u + y, t);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
