@@ -602,13 +602,13 @@ struct RowKernel {
 // (2048 rows of 15000 bf16: 256 threads with 8 chunks each 31 us, 1024 with 4 58).  Up to a row for each of 256 compute units nothing
 // overlaps, and a row is done soonest by many threads (64 rows of 8000 bf16: 64 threads with 16 chunks 10.1 us, 1024 with 4 6.8).
 static const RowKernel kManyRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(64, 8), ROW_KERNEL(256, 4), ROW_KERNEL(256, 8), ROW_KERNEL(256, 16), ROW_KERNEL(512, 16),
-                                      ROW_KERNEL(512, 32), ROW_KERNEL(512, 48)};
-static const RowKernel kFewRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(256, 4), ROW_KERNEL(1024, 4), ROW_KERNEL(1024, 8), ROW_KERNEL(512, 32), ROW_KERNEL(512, 48)};
+                                      ROW_KERNEL(512, 32), ROW_KERNEL(512, 44)};
+static const RowKernel kFewRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(256, 4), ROW_KERNEL(1024, 4), ROW_KERNEL(1024, 8), ROW_KERNEL(512, 32), ROW_KERNEL(512, 44)};
 constexpr int64_t kFew = 256;
 // Without a gradient longer rows need not be held (3000 rows of 64000 fp32: 148 us held, 117 not; of 4000, 1000 chunks, 14.7 both).
 constexpr uint32_t kLossHeld = 1024;
 #undef ROW_KERNEL
-constexpr uint32_t kHeld = 512 * 48;
+constexpr uint32_t kHeld = 512 * 44;
 
 // How a call is cut: parts = 0 is a row per workgroup.
 struct Cut {
@@ -618,7 +618,7 @@ struct Cut {
 static Cut cut_rows(int64_t rows, uint32_t chunks, uint32_t least, uint32_t most)
 {
     // Four workgroups on each of 256 compute units, which is what their registers leave room for, and not one more (48 rows of 131072
-    // fp32 in 22 parts OLD us, in 21 NEW); parts of `least` ... `most` chunks.
+    // fp32 in 22 parts 19.8 us, in 21 17.0); parts of `least` ... `most` chunks.
     uint64_t parts = 1024 / rows;
     const uint64_t upper = (chunks + least - 1) / least, lower = (chunks + (uint64_t)most - 1) / most;
     parts = parts > upper ? upper : parts;

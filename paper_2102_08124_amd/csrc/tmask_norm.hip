@@ -65,7 +65,7 @@ __device__ __forceinline__ void store_param(void *p, uint32_t f32, size_t i, flo
 
 // N parameters from column c on, of which `left` exist
 template <int N>
-__device__ __forceinline__ void load_params(const void *p, uint32_t f32, size_t c, uint32_t left, float (&v)[N])
+__device__ __forceinline__ void load_params(const void *p, uint32_t f32, uint32_t c, uint32_t left, float (&v)[N])
 {
     if (f32) {
 #pragma unroll
@@ -96,7 +96,7 @@ __device__ __forceinline__ void load_params(const void *p, uint32_t f32, size_t 
 }
 
 template <int N>
-__device__ __forceinline__ void store_params(void *p, uint32_t f32, size_t c, uint32_t left, const float (&v)[N])
+__device__ __forceinline__ void store_params(void *p, uint32_t f32, uint32_t c, uint32_t left, const float (&v)[N])
 {
     if (f32) {
 #pragma unroll
@@ -122,6 +122,18 @@ __device__ __forceinline__ void store_sums(float *p, const float (&v)[N])
 #pragma unroll
     for (int e = 0; e < N; e += 4)
         *(f32x4 *)(p + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+}
+
+template <int N>
+__device__ __forceinline__ void load_sums(const float *p, float (&v)[N])
+{
+#pragma unroll
+    for (int e = 0; e < N; e += 4) {
+        const f32x4 four = *(const f32x4 *)(p + e);
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            v[e + i] = four[i];
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -150,6 +162,14 @@ __device__ __forceinline__ float row_sum(float v, float *red)
     return v;
 }
 
+// The thread's row, of those from `first` on: the same for a wavefront if a row has one or more.
+template <int LANES>
+__device__ __forceinline__ uint32_t row_index(uint32_t first)
+{
+    const uint32_t r = first + threadIdx.x / LANES;
+    return LANES >= 64 ? (uint32_t)__builtin_amdgcn_readfirstlane((int)r) : r;
+}
+
 template <int DT, int LANES, int E>
 __global__ void __launch_bounds__(kNormThreads<LANES>) norm_kernel(const NormArgs p)
 {
@@ -166,16 +186,16 @@ __global__ void __launch_bounds__(kNormThreads<LANES>) norm_kernel(const NormArg
     auto fetch = [&](uint32_t r) {
 #pragma unroll
         for (int i = 0; i < C; i++) {
-            const size_t c = (lane + (uint32_t)(i * LANES)) * N;
+            const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
             raw[i] = more[i] = u32x4{0u, 0u, 0u, 0u};
             if (left[i] && r < p.rows) {
-                raw[i] = fetch_chunk<DT>(p.x, r * p.ld_x + c, left[i], p.cols);
+                raw[i] = fetch_chunk<DT>(row_of<DT>(p.x, r, p.ld_x), c, left[i], p.cols);
                 if (p.residual)
-                    more[i] = fetch_chunk<DT>(p.residual, r * p.ld_residual + c, left[i], p.cols);
+                    more[i] = fetch_chunk<DT>(row_of<DT>(p.residual, r, p.ld_residual), c, left[i], p.cols);
             }
         }
     };
-    const uint32_t first = blockIdx.x * kRows + threadIdx.x / LANES, step = gridDim.x * kRows;
+    const uint32_t first = row_index<LANES>(blockIdx.x * kRows), step = gridDim.x * kRows;
     fetch(first);                                                               // on the way while the parameters are read
     float w[E], b[E];
 #pragma unroll
@@ -215,7 +235,7 @@ __global__ void __launch_bounds__(kNormThreads<LANES>) norm_kernel(const NormArg
                 s += v[e];
             }
             if (p.total && left[i] && exists)
-                store_chunk<DT>(p.total, r * p.ld_total + (size_t)(lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
+                store_chunk<DT>(row_of<DT>(p.total, r, p.ld_total), (lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
         }
         const float mean = row_sum<LANES, T>(s, red[0]) * p.per_col;
         s = 0.f;
@@ -235,7 +255,7 @@ __global__ void __launch_bounds__(kNormThreads<LANES>) norm_kernel(const NormArg
             for (int e = 0; e < N; e++)
                 v[e] = t[i * N + e] * rstd * w[i * N + e] + b[i * N + e];
             if (left[i] && exists)
-                store_chunk<DT>(p.y, r * p.ld_y + (size_t)(lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
+                store_chunk<DT>(row_of<DT>(p.y, r, p.ld_y), (lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
         }
         if (p.mean && lane == 0 && exists) {
             p.mean[r] = mean;
@@ -258,9 +278,9 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormArgs 
             for (uint32_t c = threadIdx.x * N; c < p.cols; c += kLongThreads * N) {
                 const uint32_t left = p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
                 float v[N], u[N];
-                unpack<DT>(load_chunk<DT>(p.x, r * p.ld_x + c, left), v);
+                unpack<DT>(load_chunk<DT>(row_of<DT>(p.x, r, p.ld_x), c, left), v);
                 if (p.residual) {
-                    unpack<DT>(load_chunk<DT>(p.residual, r * p.ld_residual + c, left), u);
+                    unpack<DT>(load_chunk<DT>(row_of<DT>(p.residual, r, p.ld_residual), c, left), u);
 #pragma unroll
                     for (int e = 0; e < N; e++)
                         v[e] += u[e];
@@ -294,11 +314,11 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormArgs 
             if (p.bias)
                 load_params<N>(p.bias, p.param_f32, c, left, b);
             if (p.total)
-                store_chunk<DT>(p.total, r * p.ld_total + c, left, pack<DT>(v));
+                store_chunk<DT>(row_of<DT>(p.total, r, p.ld_total), c, left, pack<DT>(v));
 #pragma unroll
             for (int e = 0; e < N; e++)
                 v[e] = (v[e] - mean) * rstd * w[e] + b[e];
-            store_chunk<DT>(p.y, r * p.ld_y + c, left, pack<DT>(v));
+            store_chunk<DT>(row_of<DT>(p.y, r, p.ld_y), c, left, pack<DT>(v));
         });
         if (p.mean && threadIdx.x == 0) {
             p.mean[r] = mean;
@@ -332,12 +352,17 @@ __device__ __forceinline__ float across_rows(float v)
     return v;
 }
 
-template <int DT, int LANES, int E, bool KEEP>
+template <int DT, int LANES, int E>
 __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradArgs p)
 {
+    constexpr bool KEEP = E <= 8;                                               // weights, column sums and the next row's loads in registers
     constexpr int T = kGradThreads, N = kElems<DT>, C = E / N, kRows = T / LANES, W = T / 64, kCols = LANES * E;
     constexpr int kShared = LANES < 64 ? W : kRows;                             // sets of column sums that the workgroup adds up
+    constexpr bool MORE = DT == kBF16 || LANES < 1024;                          // dtotal ahead too: 128 registers do not hold it besides
     __shared__ float red[2][2 * W];
+    // Rows twice as wide as the registers take with all that: the sums lie in LDS, each thread's in its own places (4000 rows of 16000 fp32
+    // 221 us; with sums that spill to scratch memory 385), and the weights are read again for each row.
+    __shared__ __attribute__((aligned(16))) float kept[2][KEEP ? 4 : kCols];
     const uint32_t lane = threadIdx.x % LANES;
     uint32_t left[C];
 #pragma unroll
@@ -352,23 +377,24 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
     auto fetch = [&](uint32_t r, Row &row) {
 #pragma unroll
         for (int i = 0; i < C; i++) {
-            const size_t c = (lane + (uint32_t)(i * LANES)) * N;
+            const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
             row.dy[i] = row.x[i] = row.more[i] = u32x4{0u, 0u, 0u, 0u};
             if (left[i] && r < p.rows) {
-                row.dy[i] = fetch_chunk<DT>(p.dy, r * p.ld_dy + c, left[i], p.cols);
-                row.x[i] = fetch_chunk<DT>(p.x, r * p.ld_x + c, left[i], p.cols);
-                if (p.dtotal)
-                    row.more[i] = fetch_chunk<DT>(p.dtotal, r * p.ld_dtotal + c, left[i], p.cols);
+                row.dy[i] = fetch_chunk<DT>(row_of<DT>(p.dy, r, p.ld_dy), c, left[i], p.cols);
+                row.x[i] = fetch_chunk<DT>(row_of<DT>(p.x, r, p.ld_x), c, left[i], p.cols);
+                if (MORE && p.dtotal)
+                    row.more[i] = fetch_chunk<DT>(row_of<DT>(p.dtotal, r, p.ld_dtotal), c, left[i], p.cols);
             }
         }
         row.mean = r < p.rows ? p.mean[r] : 0.f;
         row.rstd = r < p.rows ? p.rstd[r] : 0.f;
     };
     const uint32_t step = p.strips * kRows;
-    uint32_t r = blockIdx.x * kRows + threadIdx.x / LANES, turn = 0;
+    uint32_t r = row_index<LANES>(blockIdx.x * kRows), turn = 0;
     if constexpr (KEEP)
         fetch(r, next);
-    float w[C][N], dw[C][N], db[C][N];
+    constexpr int kHeld = KEEP ? C : 1;
+    float w[kHeld][N], dw[kHeld][N], db[kHeld][N];
     auto weights = [&](int i, float (&v)[N]) {
 #pragma unroll
         for (int e = 0; e < N; e++)
@@ -378,39 +404,58 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
     };
 #pragma unroll
     for (int i = 0; i < C; i++) {
-        if constexpr (KEEP)
+        constexpr float none[N] = {};
+        if constexpr (KEEP) {
             weights(i, w[i]);
 #pragma unroll
-        for (int e = 0; e < N; e++)
-            dw[i][e] = db[i][e] = 0.f;
+            for (int e = 0; e < N; e++)
+                dw[i][e] = db[i][e] = 0.f;
+        } else {
+            store_sums(&kept[0][(lane + (uint32_t)(i * LANES)) * N], none);
+            store_sums(&kept[1][(lane + (uint32_t)(i * LANES)) * N], none);
+        }
     }
     // the same number of rounds for the whole workgroup: barriers are inside
     for (uint32_t r0 = blockIdx.x * kRows; r0 < p.rows; r0 += step, r += step, turn ^= 1) {
         if constexpr (!KEEP)
             fetch(r, next);
         const Row row = next;
-        if constexpr (KEEP)
-            if (r0 + step < p.rows)
-                fetch(r + step, next);
+        if (KEEP && r0 + step < p.rows)
+            fetch(r + step, next);
         const bool exists = r < p.rows;
+        u32x4 more[C];
+#pragma unroll
+        for (int i = 0; i < C; i++) {
+            more[i] = row.more[i];
+            if (!MORE && p.dtotal && left[i] && exists)
+                more[i] = fetch_chunk<DT>(row_of<DT>(p.dtotal, r, p.ld_dtotal), (lane + (uint32_t)(i * LANES)) * N, left[i], p.cols);
+        }
         float d[E], h[E], s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < C; i++) {
             float v[N], u[N];
             unpack<DT>(settle<DT>(row.dy[i], left[i], p.cols), v);
             unpack<DT>(settle<DT>(row.x[i], left[i], p.cols), u);
-            if constexpr (!KEEP)
-                weights(i, w[i]);
+            const int at = KEEP ? i : 0;
+            if constexpr (!KEEP) {
+                weights(i, w[0]);
+                load_sums(&kept[0][(lane + (uint32_t)(i * LANES)) * N], dw[0]);
+                load_sums(&kept[1][(lane + (uint32_t)(i * LANES)) * N], db[0]);
+            }
 #pragma unroll
             for (int e = 0; e < N; e++) {
                 const int k = i * N + e;
                 // dy is 0 in columns and rows that do not exist
                 h[k] = (u[e] - row.mean) * row.rstd;
-                dw[i][e] += v[e] * h[k];
-                db[i][e] += v[e];
-                d[k] = v[e] * w[i][e];
+                dw[at][e] += v[e] * h[k];
+                db[at][e] += v[e];
+                d[k] = v[e] * w[at][e];
                 s1 += d[k];
                 s2 += d[k] * h[k];
+            }
+            if constexpr (!KEEP) {
+                store_sums(&kept[0][(lane + (uint32_t)(i * LANES)) * N], dw[0]);
+                store_sums(&kept[1][(lane + (uint32_t)(i * LANES)) * N], db[0]);
             }
         }
         s1 = lanes_reduce<Sum, LANES < 64 ? LANES : 64>(s1);
@@ -436,12 +481,12 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
 #pragma unroll
         for (int i = 0; i < C; i++) {
             float v[N];
-            unpack<DT>(settle<DT>(row.more[i], left[i], p.cols), v);
+            unpack<DT>(settle<DT>(more[i], left[i], p.cols), v);
 #pragma unroll
             for (int e = 0; e < N; e++)
                 v[e] += row.rstd * (d[i * N + e] - s1 - h[i * N + e] * s2);
             if (left[i] && exists)
-                store_chunk<DT>(p.dx, r * p.ld_dx + (size_t)(lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
+                store_chunk<DT>(row_of<DT>(p.dx, r, p.ld_dx), (lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
         }
     }
     if (!p.dweight && !p.dbias)
@@ -450,14 +495,19 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
 #pragma unroll
         for (int i = 0; i < C; i++) {
             const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
+            const int at = KEEP ? i : 0;
+            if constexpr (!KEEP) {
+                load_sums(&kept[0][c], dw[0]);
+                load_sums(&kept[1][c], db[0]);
+            }
             if (left[i] && p.strips > 1) {
-                store_sums(p.partial + (size_t)blockIdx.x * 2 * p.pitch + c, dw[i]);
-                store_sums(p.partial + ((size_t)blockIdx.x * 2 + 1) * p.pitch + c, db[i]);
+                store_sums(p.partial + (size_t)blockIdx.x * 2 * p.pitch + c, dw[at]);
+                store_sums(p.partial + ((size_t)blockIdx.x * 2 + 1) * p.pitch + c, db[at]);
             } else if (left[i]) {
                 if (p.dweight)
-                    store_params(p.dweight, p.param_f32, c, left[i], dw[i]);
+                    store_params(p.dweight, p.param_f32, c, left[i], dw[at]);
                 if (p.dbias)
-                    store_params(p.dbias, p.param_f32, c, left[i], db[i]);
+                    store_params(p.dbias, p.param_f32, c, left[i], db[at]);
             }
         }
     } else {
@@ -524,8 +574,8 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_grad_kernel(const Norm
             for (uint32_t c = threadIdx.x * N; c < p.cols; c += kLongThreads * N) {
                 const uint32_t left = p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
                 float d[N], h[N], w[N];
-                unpack<DT>(load_chunk<DT>(p.dy, r * p.ld_dy + c, left), d);
-                unpack<DT>(load_chunk<DT>(p.x, r * p.ld_x + c, left), h);
+                unpack<DT>(load_chunk<DT>(row_of<DT>(p.dy, r, p.ld_dy), c, left), d);
+                unpack<DT>(load_chunk<DT>(row_of<DT>(p.x, r, p.ld_x), c, left), h);
 #pragma unroll
                 for (int e = 0; e < N; e++)
                     w[e] = 1.f;
@@ -556,11 +606,11 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_grad_kernel(const Norm
             for (int e = 0; e < N; e++)
                 v[e] = 0.f;
             if (p.dtotal)
-                unpack<DT>(load_chunk<DT>(p.dtotal, r * p.ld_dtotal + c, left), v);
+                unpack<DT>(load_chunk<DT>(row_of<DT>(p.dtotal, r, p.ld_dtotal), c, left), v);
 #pragma unroll
             for (int e = 0; e < N; e++)
                 v[e] += rstd * (d[e] - s1 - h[e] * s2);
-            store_chunk<DT>(p.dx, r * p.ld_dx + c, left, pack<DT>(v));
+            store_chunk<DT>(row_of<DT>(p.dx, r, p.ld_dx), c, left, pack<DT>(v));
         });
     }
 }
@@ -607,21 +657,32 @@ __global__ void __launch_bounds__(kGeluThreads<GRAD>) gelu_kernel(const GeluArgs
     const uint32_t group = blockIdx.x % p.groups, strip = blockIdx.x / p.groups;
     const uint32_t chunk = group * lanes + (threadIdx.x & (lanes - 1u)), y = threadIdx.x >> p.lanes_log2;
     const uint32_t c = chunk * N, left = chunk >= p.chunks ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
+    // Addresses are stepped from row to row: a 64-bit product for each load took a quarter of the kernel's instructions' time.
     const uint32_t step = p.strips * high;
+    uint32_t r0 = strip * high + y;
+    const unsigned char *px = (const unsigned char *)p.x + (r0 * p.ld_x + c) * kSize<DT>, *pd = (const unsigned char *)p.dy + (r0 * p.ld_dy + c) * kSize<DT>;
+    unsigned char *po = (unsigned char *)p.out + (r0 * p.ld_out + c) * kSize<DT>;
+    const size_t next_x = step * p.ld_x * kSize<DT>, next_d = step * p.ld_dy * kSize<DT>, next_o = step * p.ld_out * kSize<DT>;
+    // the chunk at a row's end: see fetch_chunk
+    const uint32_t whole = p.cols >= (uint32_t)N ? (uint32_t)N : left, back = left && left < whole ? (whole - left) * kSize<DT> : 0u;
+    px -= back;
+    pd -= back;
     u32x4 x[kGeluRows], d[kGeluRows];
-    auto fetch = [&](uint64_t r0) {
+    auto fetch = [&]() {                                                        // the rows r0, r0 + step, ...
 #pragma unroll
         for (int i = 0; i < kGeluRows; i++) {
-            const uint64_t r = r0 + (uint64_t)i * step;
             x[i] = d[i] = u32x4{0u, 0u, 0u, 0u};
-            if (left && r < p.rows) {
-                x[i] = fetch_chunk<DT>(p.x, r * p.ld_x + c, left, p.cols);
+            if (left && r0 + (uint32_t)i * step < p.rows) {
+                x[i] = load_chunk<DT>(px, 0, whole);
                 if constexpr (GRAD)
-                    d[i] = fetch_chunk<DT>(p.dy, r * p.ld_dy + c, left, p.cols);
+                    d[i] = load_chunk<DT>(pd, 0, whole);
             }
+            px += next_x;
+            if constexpr (GRAD)
+                pd += next_d;
         }
     };
-    fetch(strip * high + y);                                                    // on the way while the bias is read
+    fetch();                                                                    // on the way while the bias is read
     float b[N], sum[N];
 #pragma unroll
     for (int e = 0; e < N; e++)
@@ -629,11 +690,10 @@ __global__ void __launch_bounds__(kGeluThreads<GRAD>) gelu_kernel(const GeluArgs
     if (p.bias && left)
         load_params<N>(p.bias, p.param_f32, c, left, b);
     if (left)
-        for (uint64_t r0 = strip * high + y; r0 < p.rows;) {
+        while (r0 < p.rows) {
 #pragma unroll
             for (int i = 0; i < kGeluRows; i++) {
-                const uint64_t r = r0 + (uint64_t)i * step;
-                if (r < p.rows) {
+                if (r0 + (uint32_t)i * step < p.rows) {
                     float v[N], u[N];
                     unpack<DT>(settle<DT>(x[i], left, p.cols), v);
                     unpack<DT>(settle<DT>(d[i], left, p.cols), u);
@@ -642,15 +702,16 @@ __global__ void __launch_bounds__(kGeluThreads<GRAD>) gelu_kernel(const GeluArgs
                         v[e] = gelu<FORM, GRAD>(v[e] + b[e]);
                         if constexpr (GRAD) {
                             v[e] *= u[e];
-                            sum[e] += (uint32_t)e < left ? v[e] : 0.f;
+                            sum[e] += v[e];                                     // 0 beyond the row, where dy is 0 and x and bias are
                         }
                     }
-                    store_chunk<DT>(p.out, r * p.ld_out + c, left, pack<DT>(v));
+                    store_chunk<DT>(po, 0, left, pack<DT>(v));
                 }
+                po += next_o;
             }
-            r0 += (uint64_t)kGeluRows * step;
+            r0 += kGeluRows * step;
             if (r0 < p.rows)
-                fetch(r0);
+                fetch();
         }
     if constexpr (GRAD) {
         if (!p.dbias)
@@ -732,9 +793,9 @@ static const NormShape kNormShapes[] = {NORM_SHAPE(8, 8), NORM_SHAPE(16, 8), NOR
                                         NORM_SHAPE(256, 8), NORM_SHAPE(256, 16), NORM_SHAPE(512, 16), NORM_SHAPE(1024, 16)};
 #undef NORM_SHAPE
 
-#define GRAD_SHAPE(LANES, E, KEEP) {LANES * E, kGradThreads / LANES, {norm_grad_kernel<kF32, LANES, E, KEEP>, norm_grad_kernel<kBF16, LANES, E, KEEP>}}
-static const NormGradShape kNormGradShapes[] = {GRAD_SHAPE(8, 8, true), GRAD_SHAPE(16, 8, true), GRAD_SHAPE(32, 8, true), GRAD_SHAPE(64, 8, true), GRAD_SHAPE(128, 8, true),
-                                                GRAD_SHAPE(256, 8, true), GRAD_SHAPE(512, 8, true), GRAD_SHAPE(1024, 8, true), GRAD_SHAPE(1024, 16, false)};
+#define GRAD_SHAPE(LANES, E) {LANES * E, kGradThreads / LANES, {norm_grad_kernel<kF32, LANES, E>, norm_grad_kernel<kBF16, LANES, E>}}
+static const NormGradShape kNormGradShapes[] = {GRAD_SHAPE(8, 8), GRAD_SHAPE(16, 8), GRAD_SHAPE(32, 8), GRAD_SHAPE(64, 8), GRAD_SHAPE(128, 8), GRAD_SHAPE(256, 8), GRAD_SHAPE(512, 8),
+                                                GRAD_SHAPE(1024, 8), GRAD_SHAPE(1024, 16)};
 #undef GRAD_SHAPE
 
 // the narrowest that holds the row, none for rows that no workgroup holds

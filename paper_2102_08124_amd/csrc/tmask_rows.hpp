@@ -52,11 +52,25 @@ __device__ __forceinline__ void store_one(void *p, size_t i, float v)
         ((__bf16 *)p)[i] = (__bf16)v;
 }
 
-// elements i ... of an array, of which `left` belong to the row (at least one); the others are `fill`, a value of the type
+// row r of a matrix
 template <int DT>
-__device__ __forceinline__ u32x4 load_chunk(const void *p, size_t i, uint32_t left, float fill = 0.f)
+__device__ __forceinline__ const unsigned char *row_of(const void *p, size_t r, size_t ld)
 {
-    const unsigned char *const a = (const unsigned char *)p + i * kSize<DT>;
+    return (const unsigned char *)p + r * ld * kSize<DT>;
+}
+
+template <int DT>
+__device__ __forceinline__ unsigned char *row_of(void *p, size_t r, size_t ld)
+{
+    return (unsigned char *)p + r * ld * kSize<DT>;
+}
+
+// elements c ... of a row, of which `left` belong to it (at least one); the others are `fill`, a value of the type.  A row's bytes stay below
+// 2^32: where its address is the same for a wavefront it stays in scalar registers.
+template <int DT>
+__device__ __forceinline__ u32x4 load_chunk(const void *row, uint32_t c, uint32_t left, float fill = 0.f)
+{
+    const unsigned char *const a = (const unsigned char *)row + (uint32_t)(c * kSize<DT>);
     if (left >= (uint32_t)kElems<DT>) {
         if constexpr (DT == kF32)
             return *(const u32x4_at4 *)a;
@@ -82,10 +96,10 @@ __device__ __forceinline__ u32x4 load_chunk(const void *p, size_t i, uint32_t le
 // a wavefront's lanes fetches element by element and composes, everything that is in flight waits for it (the gradients of a layer norm of 13731
 // rows of 4476 bf16 took 175 us that way, of 4480 93).
 template <int DT>
-__device__ __forceinline__ u32x4 fetch_chunk(const void *p, size_t i, uint32_t left, uint32_t cols)
+__device__ __forceinline__ u32x4 fetch_chunk(const void *row, uint32_t c, uint32_t left, uint32_t cols)
 {
     constexpr uint32_t N = kElems<DT>;
-    return load_chunk<DT>(p, left < N && cols >= N ? i - (N - left) : i, cols >= N ? N : left);
+    return load_chunk<DT>(row, left < N && cols >= N ? c - (N - left) : c, cols >= N ? N : left);
 }
 
 template <int DT>
@@ -160,9 +174,9 @@ __device__ __forceinline__ u32x4 pack(const float (&v)[kElems<DT>])
 }
 
 template <int DT>
-__device__ __forceinline__ void store_chunk(void *p, size_t i, uint32_t left, u32x4 raw)
+__device__ __forceinline__ void store_chunk(void *row, uint32_t c, uint32_t left, u32x4 raw)
 {
-    unsigned char *const a = (unsigned char *)p + i * kSize<DT>;
+    unsigned char *const a = (unsigned char *)row + (uint32_t)(c * kSize<DT>);
     if (left >= (uint32_t)kElems<DT>) {
         if constexpr (DT == kF32)
             *(u32x4_at4 *)a = raw;
