@@ -349,8 +349,8 @@ int tmask_nm_sparse_probability(int N, int M, double rho, double *prob);
  * < 2^31 (it does not matter for a single row), rows < 2^31, cols at most 2^28 (vocab < 2^31), pointers aligned to their element type.  Any such layout
  * is taken; rows that begin at multiples of 16 bytes are read fastest.  `dt` is the type of activations and logits and of
  * their gradients, `param_dt` that of weight, bias and their gradients.  All arithmetic is in fp32 and rounded once, to nearest
- * even, where a result is stored; sums are added up in an order that depends on the sizes alone, so the same call gives the same
- * bits.  An output may be one of the call's inputs of the same type, shape and leading dimension (in place); any other overlap
+ * even, where a result is stored; sums are added up in an order that depends on the sizes (and, for the loss, on where rows
+ * begin relative to 16 bytes) and on nothing else, so the same call gives the same bits.  An output may be one of the call's inputs of the same type, shape and leading dimension (in place); any other overlap
  * is not allowed.  NaN and Inf go through the formulas.
  */
 
@@ -403,7 +403,7 @@ size_t tmask_layer_norm_workspace_bytes(int64_t rows, int64_t cols);         /* 
  *     TMASK_GELU_ERF   y = u / 2 * (1 + erf(u / sqrt 2))
  *     TMASK_GELU_TANH  y = u / 2 * (1 + tanh(sqrt(2 / pi) * (u + 0.044715 u^3)))
  * and its gradients: dx = dy * dy/du, dbias (nullable, cols elements of param_dt) = sum_rows dx, from the same x and bias.
- * Finite u give finite results, however large.  The workspace (256-byte aligned, tmask_bias_gelu_workspace_bytes(rows, cols)) is
+ * Finite u give finite results, however large, and u = +Inf gives y = +Inf.  The workspace (256-byte aligned, tmask_bias_gelu_workspace_bytes(rows, cols)) is
  * needed if dbias is asked for.
  */
 typedef enum { TMASK_GELU_ERF = 0, TMASK_GELU_TANH = 1 } tmask_gelu_form;
@@ -443,7 +443,7 @@ size_t tmask_bias_gelu_workspace_bytes(int64_t rows, int64_t cols);          /* 
  * row_max[r] = max_v z, row_sum[r] = sum_v exp((z_v - row_max) / T): nullable outputs, both or neither (q and the
  * gradient follow from them later; row_max ignores NaN).
  * dlogits is nullable: without it the call gives the loss alone.  row_weight (nullable: 1) is the weight of the row's loss in what is
- * differentiated, such as 1 / tokens.  teacher is of teacher_dt, index of 32 or 64 bits (index_bits).  0 <= k <= 1024; 0 < T, finite.
+ * differentiated, such as 1 / tokens.  teacher is of teacher_dt, index of 32 or 64 bits (index_bits).  0 <= k <= 1024; 1e-18 <= T <= 1e18.
  * The workspace (256-byte aligned, tmask_distill_workspace_bytes(rows, vocab), which is 0 for sizes that need none) serves
  * tmask_distill alone.
  */

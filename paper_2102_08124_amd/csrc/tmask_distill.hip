@@ -261,18 +261,19 @@ __device__ __forceinline__ u32x4 pull(const DistillArgs &a, u32x4 raw, float z_m
     return pack<DT>(v);
 }
 
-// Turns the logits of a thread's entries into probabilities (part of the teacher's sum, which is 1 / part and whose logarithm is t_log); the
-// result is what they add to the loss, without T^2.
-template <uint32_t T>
+// Turns the logits of a thread's entries into probabilities; the result is what they add to the loss, without T^2.
+template <uint32_t T, bool LOSS = true>
 __device__ __forceinline__ float take_entries(const DistillArgs &a, const List &list, float t_max, float t_sum, float z_max, float z_sum)
 {
-    const float t_log = logf(t_sum), z_log = logf(z_sum), part = 1.f / t_sum;
+    const float t_log = LOSS ? logf(t_sum) : 0.f, z_log = LOSS ? logf(z_sum) : 0.f, part = 1.f / t_sum;
     float loss = 0.f;
     for (uint32_t j = threadIdx.x; j < a.k; j += T)
         if (list.at[j] >= 0) {
             const float t = list.t[j] - t_max, p = exp_of(a, t) * part;
-            const float log_q = (list.z[j] - z_max) * a.per_t - z_log;
-            loss += log_q == -INFINITY ? INFINITY : p * ((t * a.per_t - t_log) - log_q);
+            if constexpr (LOSS) {
+                const float log_q = (list.z[j] - z_max) * a.per_t - z_log;
+                loss += log_q == -INFINITY ? INFINITY : p * ((t * a.per_t - t_log) - log_q);
+            }
             list.t[j] = p;
         }
     return loss;
@@ -552,9 +553,12 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
         t_sum = entries_sum<kSlice>(a, list, t_max);
         group_reduce<Sum, Sum, W>(t_sum, unused, red + 2 * W);
         const bool some = t_max != -INFINITY;
-        const float loss = lanes_reduce<Sum, 64>(take_entries<kSlice>(a, list, t_max, t_sum, z_max, z_sum));
-        if ((threadIdx.x & 63) == 0)
-            red[4 * W + (threadIdx.x >> 6)] = loss;
+        const float loss = take_entries<kSlice, JOIN>(a, list, t_max, t_sum, z_max, z_sum);
+        if constexpr (JOIN) {
+            const float sum = lanes_reduce<Sum, 64>(loss);
+            if ((threadIdx.x & 63) == 0)
+                red[4 * W + (threadIdx.x >> 6)] = sum;
+        }
         __syncthreads();
         if (JOIN && p.part == 0 && threadIdx.x == 0)
             write_row<W>(a, p.r, red + 4 * W, some, z_max, z_sum);
@@ -603,7 +607,7 @@ struct RowKernel {
 // overlaps, and a row is done soonest by many threads (64 rows of 8000 bf16: 64 threads with 16 chunks 10.1 us, 1024 with 4 6.8).
 static const RowKernel kManyRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(64, 8), ROW_KERNEL(256, 4), ROW_KERNEL(256, 8), ROW_KERNEL(256, 16), ROW_KERNEL(512, 16),
                                       ROW_KERNEL(512, 32), ROW_KERNEL(512, 44)};
-static const RowKernel kFewRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(256, 4), ROW_KERNEL(1024, 4), ROW_KERNEL(1024, 8), ROW_KERNEL(512, 32), ROW_KERNEL(512, 44)};
+static const RowKernel kFewRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(256, 4), ROW_KERNEL(1024, 4), ROW_KERNEL(1024, 8)};
 constexpr int64_t kFew = 256;
 // Without a gradient longer rows need not be held (3000 rows of 64000 fp32: 148 us held, 117 not; of 4000, 1000 chunks, 14.7 both).
 constexpr uint32_t kLossHeld = 1024;
@@ -654,8 +658,8 @@ static int check_distill(const tmask_distill_desc *desc, tmask_dtype dt, tmask_d
         return fail(TMASK_ERR_DTYPE, "unknown dtype %d, teacher's dtype %d or index of %d bits", (int)dt, (int)teacher_dt, index_bits);
     if (!valid_sizes(d.rows, d.vocab) || d.k < 0 || d.k > (int64_t)kMaxEntries)
         return fail(TMASK_ERR_SHAPE, "rows=%lld vocab=%lld k=%lld (at most %u)", (long long)d.rows, (long long)d.vocab, (long long)d.k, kMaxEntries);
-    if (!(temperature > 0.f) || std::isinf(temperature))
-        return fail(TMASK_ERR_SHAPE, "temperature=%g must be finite and positive", (double)temperature);
+    if (!(temperature >= 1e-18f && temperature <= 1e18f))                       // its square and its reciprocal are numbers
+        return fail(TMASK_ERR_SHAPE, "temperature=%g must lie between 1e-18 and 1e18", (double)temperature);
     if (d.rows == 0)
         return TMASK_OK;
     TMASK_TRY(check_rows("logits", d.logits, d.ld_logits, d.rows, d.vocab, size_of(dt), true));

@@ -2076,6 +2076,6 @@ int tmask_profile_next(void *start_event, void *stop_event)
 
 const char *tmask_last_error(void) { return g_err; }
 
-int tmask_version(void) { return 100; }
+int tmask_version(void) { return 110; }
 
 }  // extern "C"

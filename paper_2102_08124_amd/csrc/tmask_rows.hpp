@@ -65,10 +65,10 @@ __device__ __forceinline__ unsigned char *row_of(void *p, size_t r, size_t ld)
     return (unsigned char *)p + r * ld * kSize<DT>;
 }
 
-// elements c ... of a row, of which `left` belong to it (at least one); the others are `fill`, a value of the type.  A row's bytes stay below
-// 2^32: where its address is the same for a wavefront it stays in scalar registers.
+// elements c ... of a row, of which `left` belong to it (at least one); the others are 0.  A row's bytes stay below 2^32: where its address
+// is the same for a wavefront it stays in scalar registers.
 template <int DT>
-__device__ __forceinline__ u32x4 load_chunk(const void *row, uint32_t c, uint32_t left, float fill = 0.f)
+__device__ __forceinline__ u32x4 load_chunk(const void *row, uint32_t c, uint32_t left)
 {
     const unsigned char *const a = (const unsigned char *)row + (uint32_t)(c * kSize<DT>);
     if (left >= (uint32_t)kElems<DT>) {
@@ -80,11 +80,10 @@ __device__ __forceinline__ u32x4 load_chunk(const void *row, uint32_t c, uint32_
     u32x4 v;
 #pragma unroll
     for (int e = 0; e < 4; e++) {
-        const uint32_t f = __float_as_uint(fill);
         if constexpr (DT == kF32) {
-            v[e] = (uint32_t)e < left ? ((const uint32_t *)a)[e] : f;
+            v[e] = (uint32_t)e < left ? ((const uint32_t *)a)[e] : 0u;
         } else {
-            const uint32_t lo = 2u * e < left ? ((const uint16_t *)a)[2 * e] : f >> 16, hi = 2u * e + 1u < left ? ((const uint16_t *)a)[2 * e + 1] : f >> 16;
+            const uint32_t lo = 2u * e < left ? ((const uint16_t *)a)[2 * e] : 0u, hi = 2u * e + 1u < left ? ((const uint16_t *)a)[2 * e + 1] : 0u;
             v[e] = lo | hi << 16;
         }
     }

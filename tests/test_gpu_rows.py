@@ -186,6 +186,12 @@ def test_norm_grad_rows_and_parameter_types(rows, cols, dt, pdt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(600, 9000), (520, 8191), (70, 20000)])
+def test_norm_grad_several_rounds_of_wide_rows(rows, cols, dt):
+    grad_call(Maker(rows), rows, cols, dt, "f32")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("pad,shift", [(8, 0), (5, 0), (0, 1), (3, 3)])
 @pytest.mark.parametrize("cols", [37, 1024, 5000])
 def test_norm_grad_strides_and_alignment(cols, pad, shift, dt):
@@ -275,6 +281,38 @@ def test_gelu_everywhere(tanh):
         check(dx, (slope, 16 * refs.U * (1 + np.minimum(np.abs(u), 20.0))), "dx")
 
 
+@pytest.mark.parametrize("tanh", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_gelu_of_infinities(dt, tanh):
+    """+Inf passes, NaN is NaN, and the neighbours are what they were."""
+    m = Maker(16)
+    x = m.normal((3, 77), TYPES[dt])
+    y0, y = torch.empty_like(x), torch.empty_like(x)
+    tm.tmask_bias_gelu(x, y0, tanh=tanh)
+    x[1, 5], x[1, 76], x[0, 8] = float("inf"), float("nan"), float("inf")
+    tm.tmask_bias_gelu(x, y, tanh=tanh)
+    torch.cuda.synchronize()
+    assert float(y[1, 5]) == float(y[0, 8]) == float("inf") and bool(y[1, 76].isnan())
+    y0[1, 5] = y0[0, 8] = float("inf")
+    y[1, 76] = y0[1, 76]
+    assert torch.equal(y, y0)
+
+
+@pytest.mark.parametrize("T", [1e-18, 1e-3, 300.0, 1e18])
+def test_distill_temperatures(T):
+    """At the ends of their range: the coldest is the largest logit alone, the hottest the uniform distribution.  (Logits are
+    distinct integers and the loss of the hottest a difference of order 1 / T that T^2 does not bring back: gradients are compared.)"""
+    z = torch.arange(60, device="cuda", dtype=torch.float32).flip(0).reshape(1, -1)
+    teacher, index = torch.tensor([[2.0, 1.0]], device="cuda"), torch.tensor([[3, 0]], device="cuda", dtype=torch.int32)
+    loss, dz = torch.empty(1, device="cuda"), torch.empty_like(z)
+    w = torch.full((1,), 1.0 / T, device="cuda")
+    tm.tmask_distill(z, teacher, index, T, loss, dlogits=dz, row_weight=w)
+    torch.cuda.synchronize()
+    want = refs.distill(np64(z), np64(teacher), index.cpu().numpy(), T, np64(w))
+    check(dz, want["dlogits"], "dlogits")
+    assert bool(loss.isfinite().all()) or T == 1e18
+
+
 def test_gelu_in_place():
     m = Maker(4)
     x, dy = m.normal((9, 777), torch.bfloat16), m.normal((9, 777), torch.bfloat16)
@@ -337,6 +375,16 @@ def test_distill_widths(vocab, dt):
 @pytest.mark.parametrize("dt,tdt,bits,T", [("f32", "bf16", 64, 2.0), ("bf16", "f32", 32, 0.5), ("bf16", "bf16", 64, 1.0)])
 def test_distill_rows_lists_and_types(rows, vocab, k, dt, tdt, bits, T):
     distill_call(Maker(rows), rows, vocab, k, dt, tdt, bits, T, ragged=True)
+
+
+# around the lengths at which a row goes to another workgroup, to parts, or (without a gradient) through one that does not hold it
+@pytest.mark.parametrize("rows,vocab", [(70, 1026), (70, 4098), (70, 16390), (70, 32763), (70, 32779), (256, 40000), (257, 1021), (257, 1029), (257, 2050), (257, 4095),
+                                        (257, 4105), (257, 8200), (257, 16390), (257, 32775), (257, 65530), (257, 65545), (257, 90112), (257, 90117)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_distill_rows_of_every_kernel(rows, vocab, dt):
+    vocab = vocab if dt == "f32" else 2 * vocab - 1              # twice the elements to a chunk
+    z = distill_call(Maker(vocab), rows, vocab, 12, dt)[0]
+    assert z.shape == (rows, vocab)
 
 
 @pytest.mark.parametrize("k", [0, 1, 63, 64, 65, 256, 257, 1000, 1024])

@@ -68,7 +68,7 @@ for name in ("distill", "distill_grad"):
         (dict(logits=None), {}, NULL), (dict(teacher=None), {}, NULL), (dict(index=None), {}, NULL), (dict(vocab=0), {}, SHAPE), (dict(rows=-1), {}, SHAPE),
         (dict(k=-1), {}, SHAPE), (dict(k=1025, ld_teacher=2000, ld_index=2000), {}, SHAPE), (dict(ld_logits=63), {}, SHAPE), (dict(ld_teacher=7), {}, SHAPE),
         (dict(ld_index=7), {}, SHAPE), (dict(ld_dlogits=63), {}, SHAPE), ({}, dict(T=0.0), SHAPE), ({}, dict(T=-1.0), SHAPE),
-        ({}, dict(T=float("nan")), SHAPE), ({}, dict(T=float("inf")), SHAPE), ({}, dict(bits=16), DTYPE), ({}, dict(dt=5), DTYPE), ({}, dict(pdt=5), DTYPE),
+        ({}, dict(T=float("nan")), SHAPE), ({}, dict(T=float("inf")), SHAPE), ({}, dict(T=1e-19), SHAPE), ({}, dict(T=1e19), SHAPE), ({}, dict(bits=16), DTYPE), ({}, dict(dt=5), DTYPE), ({}, dict(pdt=5), DTYPE),
         (dict(logits=A + 2), {}, ALIGN), (dict(index=A + 4), dict(bits=64), ALIGN), (dict(row_weight=A + 2), {}, ALIGN), (dict(dlogits=A + 1), dict(dt=1), ALIGN)]]
 REFUSED += [("distill", dict(loss=None), {}, NULL), ("distill", dict(row_max=None), {}, NULL), ("distill", dict(row_sum=None), {}, NULL),
             ("distill", dict(loss=A + 2), {}, ALIGN), ("distill_grad", dict(row_max=None), {}, NULL), ("distill_grad", dict(row_sum=None), {}, NULL),
