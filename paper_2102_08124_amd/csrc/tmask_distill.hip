@@ -1,4 +1,9 @@
 // tmask_distill and tmask_distill_backward: the loss of a pruned model against its dense teacher's top logits, and its gradient.
+//
+// With p the teacher's distribution over a row's list, q the student's over the vocabulary, both at temperature T:
+//     loss = T^2 sum_j p_j (log p_j - log q_at(j))        dz_v = w T (q_v - sum of p_j with at(j) = v)
+// Exponentials are of differences from the row's maximum, times log2(e) / T, by the hardware's 2^x; the differences are taken first, so
+// that logits of any size (masks of the type's lowest value) neither overflow nor cancel.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -306,10 +311,12 @@ __device__ __forceinline__ void write_row(const DistillArgs &a, uint32_t r, cons
 
 // ---------------------------------------------------------------------------------------------------------------------
 // A row in the registers of one workgroup: T threads with P chunks each.  The logits are read once, added up as they arrive, and the
-// gradient is taken from the registers.
+// gradient is taken from the registers.  Bound by memory: 4096 rows of 32000 bf16, loss and gradient, 104 us (524 MB, 5.0 TB/s,
+// a device copy's rate; the vector ALU is busy for half of that time).  Logits and gradient pass with streaming loads and stores (with plain
+// ones 119 us).
 //
 // The gradient's columns that the list names are written again, with what the teacher takes from them, when the rest has been
-// written: k of the vocabulary's columns, and the barrier between orders the two.
+// written: k of the vocabulary's columns, and the barrier between orders the two (the counters see 4 % more bytes written).
 // ---------------------------------------------------------------------------------------------------------------------
 template <int DT, int T, int P>
 __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
@@ -389,7 +396,8 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
 // ---------------------------------------------------------------------------------------------------------------------
 // Few rows, or rows that no workgroup holds: parts of rows.  The first launch takes the maximum and the sum of each part and the
 // student's logits of the entries in it; the second joins them and does the rest, part by part, from logits that the caches may
-// still hold.
+// still hold.  48 rows of 131072 fp32, loss and gradient: 7 and 10 us (25 MB read, then 25 read from the caches and 25 written).
+// A gradient alone has its statistics and needs the second launch only: 1003 rows of 50021 bf16 43 us (4.6 TB/s).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kAhead = 8;                 // chunks that a thread has in flight
 

@@ -139,7 +139,9 @@ __device__ __forceinline__ void load_sums(const float *p, float (&v)[N])
 // ---------------------------------------------------------------------------------------------------------------------
 // Layer norm of rows that stay in registers: LANES lanes (a part of a wavefront, or a workgroup of several) with E elements each,
 // in chunks of 16 bytes that alternate between the lanes.  The mean first, then the mean of the squared differences
-// from it: both from registers, so that a large mean costs no digits and nothing is read twice.
+// from it: both from registers, so that a large mean costs no digits and nothing is read twice.  Bound by memory: 8192 rows of 1024 bf16
+// with a residual and its sum take 12.5 us (67 MB, 5.4 TB/s, part of it from the memory-side cache), 13731 rows 24 (112 MB, 4.7); one row 3.2 us, a launch.
+// More lanes with fewer elements each need a barrier for a row and were slower (13731 x 1024: 26 us).
 // ---------------------------------------------------------------------------------------------------------------------
 template <int LANES>
 constexpr int kNormThreads = LANES <= 256 ? 256 : LANES;
@@ -328,9 +330,12 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormArgs 
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Its gradients, with rows held the same way.  A workgroup, one on a compute unit, goes through every strips-th group of rows and keeps the sums over
-// them of dy h and dy in registers, a column in the same lane all the time; at its end the lanes and wavefronts that share
-// a column add up in LDS, and the strips' sums are added up by columns_kernel.  Rows are loaded one ahead.
+// Its gradients, with rows held the same way.  A workgroup, one on a compute unit, goes through every strips-th group of rows and keeps
+// the sums over them of dy h and dy in registers, a column in the same lane all the time; at its end the lanes and wavefronts that share
+// a column add up in LDS, and the strips' sums are added up by columns_kernel.  Rows are loaded one ahead.  Bound by memory where
+// rows are many (8192 x 1024 bf16 with dtotal: 13.5 us and 2 for the sums, 4.4 TB/s of what has to be moved; 30000 x 1024 49 us, 5.0), by the rounds'
+// and the second launch's latencies where they are few (200 x 1024: 7.3 us).  Twice the strips with half the threads move twice the sums
+// (1000 x 4096 bf16: 22 us, like this 13).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kGradThreads = 1024;
 constexpr uint32_t kGradStrips = 256;
@@ -618,8 +623,11 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_grad_kernel(const Norm
 // ---------------------------------------------------------------------------------------------------------------------
 // GELU.  With E(a) = exp(-a^2 / 2), the share Phi(u) = (1 + erf(u / sqrt 2)) / 2 that passes is E(u) R(t) for u < 0 and one minus that of -u for
 // u > 0, t = 1 / (1 + 0.33 |u|): R is the polynomial of degree 5 without constant term for which E R differs least from
-// the share over all u (by 4.2e-8, fitted by linear programming; 1.8e-7 with the roundings of fp32).  The derivative Phi(u) + u E(u) / sqrt(2 pi) has the same exponential.  The form with
-// tanh is the share 1 / (1 + exp(-2 s)).
+// the share over all u (by 4.2e-8, fitted by linear programming; 1.8e-7 with the roundings of fp32).  The derivative Phi(u) + u E(u) / sqrt(2 pi)
+// has the same exponential.  The form with tanh is the share 1 / (1 + exp(-2 s)).
+//
+// Bound by memory at size, with the vector ALU not far behind: 8192 x 4096 bf16 28.8 us (134 MB, 4.7 TB/s; 16 instructions an element, of which two
+// transcendentals that take four times as long), gradients 43.7 us (201 MB, 4.6 TB/s; 21 instructions).  A library erf instead took 57 us.
 // ---------------------------------------------------------------------------------------------------------------------
 template <int FORM, bool GRAD>
 __device__ __forceinline__ float gelu(float u)
@@ -642,8 +650,8 @@ __device__ __forceinline__ float gelu(float u)
     }
 }
 
-// Workgroups of 256 threads (1024 for gradients, to have fewer strips) as 2^lanes_log2 lanes of a chunk each by the rest of the rows; a thread keeps its columns (and their
-// bias and, for gradients, their sums) and takes kGeluRows rows at a time.
+// Workgroups of 256 threads (1024 for gradients, to have fewer strips) as 2^lanes_log2 lanes of a chunk each by the rest of the
+// rows; a thread keeps its columns (and their bias and, for gradients, their sums) and takes kGeluRows rows at a time.
 constexpr int kGeluRows = 4;
 
 template <bool GRAD>
@@ -734,7 +742,8 @@ __global__ void __launch_bounds__(kGeluThreads<GRAD>) gelu_kernel(const GeluArgs
     }
 }
 
-// Adds up the strips' sums: 8 lanes take 32 neighbouring columns (a line of 128 bytes), 32 of these groups every 32nd strip.
+// Adds up the strips' sums: 8 lanes take 32 neighbouring columns (a line of 128 bytes), 32 of these groups every 32nd strip.  Latency:
+// 3 to 4 us, whatever the size up to 256 strips of 4096 columns.
 __global__ void __launch_bounds__(kThreads) columns_kernel(const ColumnArgs p)
 {
     void *const out = p.out[blockIdx.y];
