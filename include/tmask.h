@@ -350,7 +350,7 @@ int tmask_nm_sparse_probability(int N, int M, double rho, double *prob);
  * is taken; rows that begin at multiples of 16 bytes are read fastest.  `dt` is the type of activations and logits and of
  * their gradients, `param_dt` that of weight, bias and their gradients.  All arithmetic is in fp32 and rounded once, to nearest
  * even, where a result is stored; sums are added up in an order that depends on the sizes (and, for the loss, on where rows
- * begin relative to 16 bytes) and on nothing else, so the same call gives the same bits.  An output may be one of the call's inputs of the same type, shape and leading dimension (in place); any other overlap
+ * begin relative to 16 bytes, for column sums on whether an output lies over an input) and on nothing else, so the same call gives the same bits.  An output may be one of the call's inputs of the same type, shape and leading dimension (in place); any other overlap
  * is not allowed.  NaN and Inf go through the formulas.
  */
 

@@ -32,6 +32,7 @@ struct NormGradArgs {
     uint32_t rows, cols;
     uint32_t param_f32;
     uint32_t strips, pitch;               // strips = 1: the sums go straight to dweight and dbias
+    uint32_t apart;                       // workgroups beyond the strips, which add up the columns: the strips then do not
     float per_col;
 };
 
@@ -330,11 +331,12 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormArgs 
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Its gradients, with rows held the same way.  A workgroup, one on a compute unit, goes through every strips-th group of rows and keeps
+// Its gradients, with rows held the same way.  A workgroup, one on a compute unit, goes through every strips-th group of rows and (unless the
+// batch is short: see norm_grad_columns) keeps
 // the sums over them of dy h and dy in registers, a column in the same lane all the time; at its end the lanes and wavefronts that share
 // a column add up in LDS, and the strips' sums are added up by columns_kernel.  Rows are loaded one ahead.  Bound by memory where
 // rows are many (8192 x 1024 bf16 with dtotal: 13.5 us and 2 for the sums, 4.4 TB/s of what has to be moved; 30000 x 1024 49 us, 5.0), by the rounds'
-// and the second launch's latencies where they are few (200 x 1024: 7.3 us).  Twice the strips with half the threads move twice the sums
+// latencies where they are few (1003 x 2051 fp32 11.6 us).  Twice the strips with half the threads move twice the sums
 // (1000 x 4096 bf16: 22 us, like this 13).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kGradThreads = 1024;
@@ -357,8 +359,84 @@ __device__ __forceinline__ float across_rows(float v)
     return v;
 }
 
-template <int DT, int LANES, int E>
-__global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradArgs p)
+// The column sums of a short batch by workgroups of their own, in the same launch: A lanes a row, as few as make a line of 128 bytes
+// and take half of the chip, and all rows.  They read dy and x once more, through the caches, and nothing has to be handed over or waited for.
+constexpr uint32_t kApartGroups = kGradStrips / 2;
+constexpr int64_t kApartRows = 1024;
+
+template <int DT>
+constexpr uint32_t apart_lanes(uint32_t cols)
+{
+    uint32_t a = 8;
+    while (cols > kApartGroups * a * kElems<DT>)
+        a *= 2;
+    return a;
+}
+
+template <int DT, int A>
+__device__ __forceinline__ void norm_grad_columns(const NormGradArgs &p, uint32_t group)
+{
+    constexpr int N = kElems<DT>, W = kGradThreads / 64, kAhead = 2, kWidth = A * N;
+    constexpr uint32_t kHigh = kGradThreads / A;
+    __shared__ __attribute__((aligned(16))) float sums[W][2][kWidth];
+    const uint32_t c = (group * A + threadIdx.x % A) * N, left = c >= p.cols ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
+    float dw[N], db[N];
+#pragma unroll
+    for (int e = 0; e < N; e++)
+        dw[e] = db[e] = 0.f;
+    if (left)
+        for (uint32_t r0 = threadIdx.x / A; r0 < p.rows; r0 += kAhead * kHigh) {
+            u32x4 dy[kAhead], x[kAhead];
+            float mean[kAhead], rstd[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; i++) {
+                const uint32_t r = r0 + (uint32_t)i * kHigh;
+                dy[i] = x[i] = u32x4{0u, 0u, 0u, 0u};
+                mean[i] = rstd[i] = 0.f;
+                if (r < p.rows) {
+                    dy[i] = fetch_chunk<DT>(row_of<DT>(p.dy, r, p.ld_dy), c, left, p.cols);
+                    x[i] = fetch_chunk<DT>(row_of<DT>(p.x, r, p.ld_x), c, left, p.cols);
+                    mean[i] = p.mean[r];
+                    rstd[i] = p.rstd[r];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; i++) {
+                float v[N], u[N];
+                unpack<DT>(settle<DT>(dy[i], left, p.cols), v);
+                unpack<DT>(settle<DT>(x[i], left, p.cols), u);
+#pragma unroll
+                for (int e = 0; e < N; e++) {
+                    dw[e] += v[e] * ((u[e] - mean[i]) * rstd[i]);
+                    db[e] += v[e];
+                }
+            }
+        }
+#pragma unroll
+    for (int e = 0; e < N; e++) {
+        dw[e] = across_rows<A>(dw[e]);
+        db[e] = across_rows<A>(db[e]);
+    }
+    if (threadIdx.x % 64u < A) {
+        store_sums(&sums[threadIdx.x / 64u][0][threadIdx.x % 64u * N], dw);
+        store_sums(&sums[threadIdx.x / 64u][1][threadIdx.x % 64u * N], db);
+    }
+    __syncthreads();
+    if (threadIdx.x < 2u * kWidth) {
+        const uint32_t which = threadIdx.x / kWidth, at = threadIdx.x % kWidth, col = group * kWidth + at;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; i++)
+            s += sums[i][which][at];
+        void *const out = which ? p.dbias : p.dweight;
+        if (out && col < p.cols)
+            store_param(out, p.param_f32, col, s);
+    }
+}
+
+// SUMS: with the column sums.
+template <int DT, int LANES, int E, bool SUMS>
+__device__ __forceinline__ void norm_grad_rows(const NormGradArgs p)
 {
     constexpr bool KEEP = E <= 8;                                               // weights, column sums and the next row's loads in registers
     constexpr int T = kGradThreads, N = kElems<DT>, C = E / N, kRows = T / LANES, W = T / 64, kCols = LANES * E;
@@ -367,7 +445,7 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
     __shared__ float red[2][2 * W];
     // Rows twice as wide as the registers take with all that: the sums lie in LDS, each thread's in its own places (4000 rows of 16000 fp32
     // 221 us; with sums that spill to scratch memory 385), and the weights are read again for each row.
-    __shared__ __attribute__((aligned(16))) float kept[2][KEEP ? 4 : kCols];
+    __shared__ __attribute__((aligned(16))) float kept[2][KEEP || !SUMS ? 4 : kCols];
     const uint32_t lane = threadIdx.x % LANES;
     uint32_t left[C];
 #pragma unroll
@@ -415,7 +493,7 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
 #pragma unroll
             for (int e = 0; e < N; e++)
                 dw[i][e] = db[i][e] = 0.f;
-        } else {
+        } else if constexpr (SUMS) {
             store_sums(&kept[0][(lane + (uint32_t)(i * LANES)) * N], none);
             store_sums(&kept[1][(lane + (uint32_t)(i * LANES)) * N], none);
         }
@@ -442,8 +520,9 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
             unpack<DT>(settle<DT>(row.dy[i], left[i], p.cols), v);
             unpack<DT>(settle<DT>(row.x[i], left[i], p.cols), u);
             const int at = KEEP ? i : 0;
-            if constexpr (!KEEP) {
+            if constexpr (!KEEP)
                 weights(i, w[0]);
+            if constexpr (SUMS && !KEEP) {
                 load_sums(&kept[0][(lane + (uint32_t)(i * LANES)) * N], dw[0]);
                 load_sums(&kept[1][(lane + (uint32_t)(i * LANES)) * N], db[0]);
             }
@@ -452,13 +531,15 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
                 const int k = i * N + e;
                 // dy is 0 in columns and rows that do not exist
                 h[k] = (u[e] - row.mean) * row.rstd;
-                dw[at][e] += v[e] * h[k];
-                db[at][e] += v[e];
+                if constexpr (SUMS) {
+                    dw[at][e] += v[e] * h[k];
+                    db[at][e] += v[e];
+                }
                 d[k] = v[e] * w[at][e];
                 s1 += d[k];
                 s2 += d[k] * h[k];
             }
-            if constexpr (!KEEP) {
+            if constexpr (SUMS && !KEEP) {
                 store_sums(&kept[0][(lane + (uint32_t)(i * LANES)) * N], dw[0]);
                 store_sums(&kept[1][(lane + (uint32_t)(i * LANES)) * N], db[0]);
             }
@@ -494,9 +575,9 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
                 store_chunk<DT>(row_of<DT>(p.dx, r, p.ld_dx), (lane + (uint32_t)(i * LANES)) * N, left[i], pack<DT>(v));
         }
     }
-    if (!p.dweight && !p.dbias)
+    if (!SUMS || (!p.dweight && !p.dbias))
         return;
-    if constexpr (kRows == 1) {
+    if constexpr (SUMS && kRows == 1) {
 #pragma unroll
         for (int i = 0; i < C; i++) {
             const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
@@ -515,7 +596,7 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
                     store_params(p.dbias, p.param_f32, c, left[i], db[at]);
             }
         }
-    } else {
+    } else if constexpr (SUMS) {
         __shared__ __attribute__((aligned(16))) float sums[kShared][2][kCols];
         const uint32_t set = LANES < 64 ? threadIdx.x >> 6 : threadIdx.x / LANES;
 #pragma unroll
@@ -547,6 +628,21 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradA
             }
         }
     }
+}
+
+template <int DT, int LANES, int E>
+__global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const NormGradArgs p)
+{
+    norm_grad_rows<DT, LANES, E, true>(p);
+}
+
+template <int DT, int LANES, int E>
+__global__ void __launch_bounds__(kGradThreads) norm_short_grad_kernel(const NormGradArgs p)
+{
+    if (blockIdx.x < p.strips)
+        norm_grad_rows<DT, LANES, E, false>(p);
+    else
+        norm_grad_columns<DT, (int)apart_lanes<DT>(LANES * E)>(p, blockIdx.x - p.strips);
 }
 
 // Rows that no workgroup holds: the sums over rows first (dx may lie over dy or x), a column a thread, then dx in two passes.
@@ -727,11 +823,22 @@ __global__ void __launch_bounds__(kGeluThreads<GRAD>) gelu_kernel(const GeluArgs
         __shared__ __attribute__((aligned(16))) float sums[T * N];               // [y][lane][element]
         store_sums(sums + threadIdx.x * N, sum);
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < lanes * N; i += T) {
-            const uint32_t col = group * lanes * N + i;
+        const uint32_t width = lanes * N;                                       // columns of the workgroup
+        uint32_t sets = high;
+        if (width < T) {                                                        // all threads take part first
+            sets = T / width;
             float s = 0.f;
-            for (uint32_t k = 0; k < high; k++)
-                s += sums[k * lanes * N + i];
+            for (uint32_t i = threadIdx.x; i < T * N; i += T)
+                s += sums[i];
+            __syncthreads();
+            sums[threadIdx.x] = s;
+            __syncthreads();
+        }
+        for (uint32_t i = threadIdx.x; i < width; i += T) {
+            const uint32_t col = group * width + i;
+            float s = 0.f;
+            for (uint32_t k = 0; k < sets; k++)
+                s += sums[k * width + i];
             if (col < p.cols) {
                 if (p.strips > 1)
                     p.partial[(size_t)strip * p.pitch + col] = s;
@@ -794,7 +901,8 @@ struct NormShape {
 
 struct NormGradShape {
     uint32_t cols, rows;
-    void (*kernel[2])(const NormGradArgs);
+    uint32_t apart[2];                                                          // lanes that add up a short batch's columns
+    void (*kernel[2])(const NormGradArgs), (*few[2])(const NormGradArgs);
 };
 
 #define NORM_SHAPE(LANES, E) {LANES * E, kNormThreads<LANES> / LANES, kNormThreads<LANES>, {norm_kernel<kF32, LANES, E>, norm_kernel<kBF16, LANES, E>}}
@@ -802,7 +910,10 @@ static const NormShape kNormShapes[] = {NORM_SHAPE(8, 8), NORM_SHAPE(16, 8), NOR
                                         NORM_SHAPE(256, 8), NORM_SHAPE(256, 16), NORM_SHAPE(512, 16), NORM_SHAPE(1024, 16)};
 #undef NORM_SHAPE
 
-#define GRAD_SHAPE(LANES, E) {LANES * E, kGradThreads / LANES, {norm_grad_kernel<kF32, LANES, E>, norm_grad_kernel<kBF16, LANES, E>}}
+#define GRAD_SHAPE(LANES, E)                                                                                                      \
+    {LANES * E, kGradThreads / LANES, {apart_lanes<kF32>(LANES * E), apart_lanes<kBF16>(LANES * E)},                              \
+     {norm_grad_kernel<kF32, LANES, E>, norm_grad_kernel<kBF16, LANES, E>},                                                       \
+     {norm_short_grad_kernel<kF32, LANES, E>, norm_short_grad_kernel<kBF16, LANES, E>}}
 static const NormGradShape kNormGradShapes[] = {GRAD_SHAPE(8, 8), GRAD_SHAPE(16, 8), GRAD_SHAPE(32, 8), GRAD_SHAPE(64, 8), GRAD_SHAPE(128, 8), GRAD_SHAPE(256, 8), GRAD_SHAPE(512, 8),
                                                 GRAD_SHAPE(1024, 8), GRAD_SHAPE(1024, 16)};
 #undef GRAD_SHAPE
@@ -818,6 +929,25 @@ static const Shape *shape_for(const Shape (&shapes)[n], int64_t cols)
 }
 
 static uint32_t at_most(uint64_t v, uint32_t most) { return (uint32_t)(v < most ? v : most); }
+
+// whether two tensors of a call may share memory
+static bool overlaps(const void *a, int64_t ld_a, const void *b, int64_t ld_b, int64_t rows, int64_t cols, size_t size)
+{
+    const uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
+    return pa < pb + (size_t)((rows - 1) * ld_b + cols) * size && pb < pa + (size_t)((rows - 1) * ld_a + cols) * size;
+}
+
+// Column sums by workgroups of their own: 200 rows of 1024 bf16 4.7 us (two launches 7.2), of 12000 9.3 (16.3), 1003 of 2051 fp32 11.6 (12.7), of
+// 12000 bf16 31 (36), but 1500 of 1024 10.3 (7.7).  Not where a workgroup would write what another reads.
+static bool columns_apart(const tmask_norm_grad_desc &d, size_t size, size_t psize)
+{
+    if (d.rows > kApartRows)
+        return false;
+    for (void *const sums : {d.dweight, d.dbias})
+        if (sums && ((d.weight && overlaps(sums, 0, d.weight, 0, 1, d.cols, psize)) || sums == d.mean || sums == d.rstd))
+            return false;
+    return !overlaps(d.dx, d.ld_dx, d.dy, d.ld_dy, d.rows, d.cols, size) && !overlaps(d.dx, d.ld_dx, d.x, d.ld_x, d.rows, d.cols, size);
+}
 
 static uint32_t pitch_of(int64_t cols) { return (uint32_t)((cols + 7) & ~7ll); }      // whole chunks of either type
 
@@ -853,16 +983,27 @@ static void gelu_tile(int64_t rows, int64_t cols, tmask_dtype dt, bool grad, Gel
             best = l;
         }
     }
-    p->lanes_log2 = best;
-    p->groups = (p->chunks + (1u << best) - 1) >> best;
-    const uint64_t high = (grad ? kGradThreads : kThreads) >> best;
-    // Gradients: up to 16 elements a thread, a second launch costs more than workgroups beside each other alone (16 rows of 1024 bf16
-    // 5.3 and 7.0 us; 32 elements 8.4 and 7.0).
-    // (Of the gradients' workgroups a compute unit holds one: one more than there are units doubles the time.)
-    const uint64_t rounds = (rows + high - 1) / high, all = grad ? kGradStrips : 2048, most = p->groups < all ? all / p->groups : 1;
-    const uint64_t each = grad && rounds * n <= 16 ? 16 / n : rounds <= most ? 1 : grad ? (rounds + most - 1) / most : 0;
-    p->strips = (uint32_t)(each ? (rounds + each - 1) / each : most);
+    const auto lanes = [&](uint32_t log2) {
+        p->lanes_log2 = log2;
+        p->groups = (p->chunks + (1u << log2) - 1) >> log2;
+        return (rows + ((int64_t)(grad ? kGradThreads : kThreads) >> log2) - 1) / ((int64_t)(grad ? kGradThreads : kThreads) >> log2);
+    };
     p->pitch = pitch_of(cols);
+    // Gradients of a short batch: workgroups beside each other alone, few lanes to a row and so all rows in a workgroup, and no second launch.
+    // Up to 16 elements a thread, as few as there can be: 20 rows of 4096 bf16 4.2 us (two launches 7.1), 200 4.9 (7.6), 400 7.0 (8.2), with 32
+    // elements 8.9.  Four lanes (half a line each) in two rounds at most and on half of the chip: 900 rows of 1001 fp32 in four rounds
+    // 9.3 (7.2), 200 of 4096 fp32 by 256 workgroups of them 6.0, by 128 of eight lanes 4.9.
+    if (grad && rows > 0 && p->chunks < 1u << 20)
+        for (uint32_t rounds = 1; rounds * n <= 16; rounds++)
+            for (uint32_t l = best; l >= (rounds <= 2 ? 2u : 3u); l--)
+                if (lanes(l) <= rounds && p->groups <= (l == 2 ? kGradStrips / 2 : kGradStrips)) {
+                    p->strips = 1;
+                    return;
+                }
+    // (Of the gradients' workgroups a compute unit holds one: one more than there are units doubles the time.)
+    const uint64_t rounds = lanes(best), all = grad ? kGradStrips : 2048, most = p->groups < all ? all / p->groups : 1;
+    const uint64_t each = rounds <= most ? 1 : grad ? (rounds + most - 1) / most : 0;
+    p->strips = (uint32_t)(each ? (rounds + each - 1) / each : most);
 }
 
 // columns such that a launch over them stays below 2^32 threads
@@ -938,7 +1079,7 @@ extern "C" int tmask_layer_norm_backward(const tmask_norm_grad_desc *desc, tmask
     hipStream_t stream = (hipStream_t)hip_stream;
     const uint32_t strips = norm_strips(d.rows, d.cols);
     NormGradArgs p{d.dy, d.x, d.weight, d.dtotal, d.mean, d.rstd, d.dx, d.dweight, d.dbias, (float *)workspace, (size_t)d.ld_dy, (size_t)d.ld_x,
-                   (size_t)d.ld_dtotal, (size_t)d.ld_dx, (uint32_t)d.rows, (uint32_t)d.cols, param_dt == TMASK_F32, strips, pitch_of(d.cols),
+                   (size_t)d.ld_dtotal, (size_t)d.ld_dx, (uint32_t)d.rows, (uint32_t)d.cols, param_dt == TMASK_F32, strips, pitch_of(d.cols), 0,
                    (float)(1.0 / (double)d.cols)};
     const NormGradShape *const shape = shape_for(kNormGradShapes, d.cols);
     if (d.rows > 0) {
@@ -952,7 +1093,12 @@ extern "C" int tmask_layer_norm_backward(const tmask_norm_grad_desc *desc, tmask
         if (sums)
             TMASK_TRY(check_workspace(workspace, workspace_bytes, tmask_layer_norm_workspace_bytes(d.rows, d.cols)));
         if (shape) {
-            hipLaunchKernelGGL(shape->kernel[dt], dim3(strips), dim3(kGradThreads), 0, stream, p);
+            if (sums && columns_apart(d, size, psize)) {
+                const uint32_t width = shape->apart[dt] * (uint32_t)(16 / size);
+                p.apart = ((uint32_t)d.cols + width - 1) / width;
+                p.strips = at_most((d.rows + shape->rows - 1) / shape->rows, kGradStrips - p.apart);
+            }
+            hipLaunchKernelGGL(p.apart ? shape->few[dt] : shape->kernel[dt], dim3(p.strips + p.apart), dim3(kGradThreads), 0, stream, p);
         } else {
             if (sums)
                 hipLaunchKernelGGL(dt == TMASK_F32 ? norm_long_columns_kernel<kF32> : norm_long_columns_kernel<kBF16>,
@@ -961,7 +1107,7 @@ extern "C" int tmask_layer_norm_backward(const tmask_norm_grad_desc *desc, tmask
                                dim3(kLongThreads), 0, stream, p);
         }
     }
-    if (sums && (strips != 1 || !shape))
+    if (sums && !p.apart && (strips != 1 || !shape))
         sum_columns(p.partial, d.dweight, d.dbias, d.cols, strips, 2, param_dt, stream);
     return launched("layer norm gradient launch");
 }

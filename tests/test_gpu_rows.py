@@ -204,6 +204,35 @@ def test_norm_grad_without_its_options(cols, more, affine):
     grad_call(Maker(5), 4, cols, "bf16", "f32", more, affine)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [60, 500, 1027, 4096, 4101, 8192, 8197, 16384])
+@pytest.mark.parametrize("rows", [31, 257, 700, 1024, 1025])
+def test_norm_grad_of_short_batches(rows, cols, dt):
+    """Both sides of the sizes at which column sums have workgroups of their own, at every width of these."""
+    grad_call(Maker(rows), rows, cols, dt, "f32", more=rows % 2 == 1)
+
+
+@pytest.mark.parametrize("in_place", ["dy", "x"])
+@pytest.mark.parametrize("dt,rows,cols", [("f32", 700, 1000), ("bf16", 1024, 2048), ("bf16", 40, 9000)])
+def test_norm_grad_of_short_batches_in_place(dt, rows, cols, in_place):
+    grad_call(Maker(rows), rows, cols, dt, "f32", in_place=in_place)
+
+
+@pytest.mark.parametrize("over", ["weight", "mean", "rstd"])
+@pytest.mark.parametrize("which", ["dweight", "dbias"])
+def test_norm_grad_of_a_parameter_over_what_is_read(which, over):
+    n = 300                                                                     # rows and columns: statistics and parameters have one shape
+    m = Maker(12)
+    x, dy, w = m.normal((n, n), torch.float32), m.normal((n, n), torch.float32), m.normal((n,), torch.float32, 0.2, 1.0)
+    read = {"weight": w, "mean": x.mean(1), "rstd": (x.var(1, correction=0) + 1e-5).rsqrt()}
+    want = refs.layer_norm_backward(np64(dy), np64(x), np64(read["mean"]), np64(read["rstd"]), np64(w), None)
+    dx, ws = torch.empty_like(x), tm.alloc_layer_norm_workspace(x)
+    tm.tmask_layer_norm_backward(dy, x, read["mean"], read["rstd"], dx, w, workspace=ws, **{which: read[over]})
+    torch.cuda.synchronize()
+    check(dx, want["dx"], "dx")
+    check(read[over], want[which], which)
+
+
 @pytest.mark.parametrize("in_place", ["dy", "x", "dtotal"])
 @pytest.mark.parametrize("cols", [300, 1024, 3000, 20000])
 def test_norm_grad_in_place(cols, in_place):
@@ -252,6 +281,14 @@ def test_gelu_widths(cols, dt, tanh):
 @pytest.mark.parametrize("rows,cols", [(2, 1024), (1003, 130), (700, 1024), (33, 4100), (9000, 40)])
 def test_gelu_rows_and_parameter_types(rows, cols, dt, pdt):
     gelu_call(Maker(rows), rows, cols, dt, pdt, rows % 2 == 0)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [12, 64, 704, 1001, 4096, 12007])
+@pytest.mark.parametrize("rows", [16, 20, 129, 256, 257, 400, 512, 513])
+def test_gelu_of_short_batches(rows, cols, dt):
+    """Both sides of the sizes at which a workgroup of the gradients has all rows."""
+    gelu_call(Maker(rows), rows, cols, dt, "f32", False)
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])

@@ -13,6 +13,14 @@ def test_gradients_have_a_workgroup_of_1024_threads_on_a_compute_unit(kernels): 
         assert use["scratch"] <= (80 if name == "norm_grad_kernel<0, 1024, 16>" else 0), (name, use)
 
 
+def test_gradients_of_short_batches_have_a_compute_unit_too(kernels):       # noqa: F811
+    found = {name: use for name, uses in kernels.items() for use in uses if name.startswith("norm_short_grad_kernel<")}
+    assert len(found) == 18
+    for name, use in found.items():
+        assert use["threads"] == 1024 and use["vgpr"] <= 128 and use["lds"] <= 160 * 1024, (name, use)
+        assert use["scratch"] <= (32 if name == "norm_short_grad_kernel<0, 1024, 16>" else 0), (name, use)
+
+
 def test_forward_row_kernels_use_no_scratch_memory(kernels):       # noqa: F811
     found = {name: use for name, uses in kernels.items() for use in uses if re.match(r"norm_(long_)?kernel<|norm_long_|gelu_kernel<\d, \d, false>|columns_kernel", name)}
     assert len(found) == 18 + 2 + 4 + 4 + 1
