@@ -606,16 +606,21 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
 // ---------------------------------------------------------------------------------------------------------------------
 struct RowKernel {
     uint32_t threads, chunks;                                                   // that the workgroup holds
+    int64_t above;                                                              // for calls of more rows than this
     void (*kernel[2])(const DistillArgs);
 };
 
-#define ROW_KERNEL(T, P) {T, T * P, {distill_row_kernel<kF32, T, P>, distill_row_kernel<kBF16, T, P>}}
+#define ROW_KERNEL(T, P, ABOVE) {T, T * P, ABOVE, {distill_row_kernel<kF32, T, P>, distill_row_kernel<kBF16, T, P>}}
 // A compute unit holds several of the smaller workgroups, which overlap one row's loads with another's arithmetic: with many rows they win
 // (2048 rows of 15000 bf16: 256 threads with 8 chunks each 31 us, 1024 with 4 58).  Up to a row for each of 256 compute units nothing
-// overlaps, and a row is done soonest by many threads (64 rows of 8000 bf16: 64 threads with 16 chunks 10.1 us, 1024 with 4 6.8).
-static const RowKernel kManyRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(64, 8), ROW_KERNEL(256, 4), ROW_KERNEL(256, 8), ROW_KERNEL(256, 16), ROW_KERNEL(512, 16),
-                                      ROW_KERNEL(512, 32), ROW_KERNEL(512, 44)};
-static const RowKernel kFewRows[] = {ROW_KERNEL(64, 4), ROW_KERNEL(256, 4), ROW_KERNEL(1024, 4), ROW_KERNEL(1024, 8)};
+// overlaps, and a row is done soonest by many threads (64 rows of 8000 bf16: 64 threads with 16 chunks 10.1 us, 1024 with 4 6.8).  In between
+// the chip takes so many wavefronts of a row at once: 4000 rows of 2304 fp32 by 256 threads 24.4 us, by 64 17.7, but 400 rows 6.6 and 7.4; 2000 of
+// 9000 bf16 by 256 threads 23.1, by 128 20.1, 400 of 10000 9.2 and 10.7; 300 of 2304 bf16 by 64 threads 7.1, by 256 6.6, 800 7.5 and 8.0.
+// The first that holds the row and is for so many.
+static const RowKernel kManyRows[] = {ROW_KERNEL(64, 4, 0), ROW_KERNEL(64, 8, 640), ROW_KERNEL(64, 12, 1536), ROW_KERNEL(128, 8, 1536), ROW_KERNEL(256, 4, 0),
+                                      ROW_KERNEL(128, 12, 640), ROW_KERNEL(256, 8, 0), ROW_KERNEL(256, 16, 0), ROW_KERNEL(512, 16, 0), ROW_KERNEL(512, 32, 0),
+                                      ROW_KERNEL(512, 44, 0)};
+static const RowKernel kFewRows[] = {ROW_KERNEL(64, 4, 0), ROW_KERNEL(256, 4, 0), ROW_KERNEL(1024, 4, 0), ROW_KERNEL(1024, 8, 0)};
 constexpr int64_t kFew = 256;
 // Without a gradient longer rows need not be held (3000 rows of 64000 fp32: 148 us held, 117 not; of 4000, 1000 chunks, 14.7 both).
 constexpr uint32_t kLossHeld = 1024;
@@ -729,7 +734,7 @@ extern "C" int tmask_distill(const tmask_distill_desc *desc, tmask_dtype dt, tma
                            stream, a);
     } else if (cut.parts == 0) {
         const RowKernel *k = desc->rows <= kFew ? kFewRows : kManyRows;
-        while (k->chunks < chunks_of(desc->vocab, dt))
+        while (k->chunks < chunks_of(desc->vocab, dt) || desc->rows <= k->above)
             k++;
         hipLaunchKernelGGL(k->kernel[bf16], dim3(grid_of(a.rows)), dim3(k->threads), 20 * (k->threads / 64) + list, stream, a);
     } else {

@@ -30,7 +30,7 @@ def test_forward_row_kernels_use_no_scratch_memory(kernels):       # noqa: F811
 
 def test_a_row_held_in_registers_is_held_there(kernels):       # noqa: F811
     found = {name: use for name, uses in kernels.items() for use in uses if name.startswith("distill_")}
-    assert len(found) == 2 * 10 + 2 + 2 + 4
+    assert len(found) == 2 * 13 + 2 + 2 + 4
     for name, use in found.items():
         assert use["scratch"] == 0, (name, use)
     # four workgroups of the kernels that work on parts of rows on a compute unit: what rows are cut by
