@@ -346,12 +346,13 @@ int tmask_nm_sparse_probability(int N, int M, double rho, double *prob);
  * A sparse model is trained, or recovered from its dense teacher, by steps whose products tmask_spmm24 computes; the
  * calls below are what such a step does between them, forward and backward, and its loss.  They work on rows of any width:
  * rows >= 0, cols > 0 (rows = 0: nothing is done, and column sums are 0), every leading dimension >= the row's width and
- * < 2^31 (it does not matter for a single row), rows < 2^31, cols at most 2^28 (vocab < 2^31), pointers aligned to their element type.  Any such layout
- * is taken; rows that begin at multiples of 16 bytes are read fastest.  `dt` is the type of activations and logits and of
+ * < 2^31 (it does not matter for a single row), rows < 2^31, cols at most 2^28 (vocab < 2^31), pointers aligned to their element
+ * type.  Any such layout is taken; rows that begin at multiples of 16 bytes are read fastest.  `dt` is the type of activations and logits and of
  * their gradients, `param_dt` that of weight, bias and their gradients.  All arithmetic is in fp32 and rounded once, to nearest
  * even, where a result is stored; sums are added up in an order that depends on the sizes (and, for the loss, on where rows
- * begin relative to 16 bytes, for column sums on whether an output lies over an input) and on nothing else, so the same call gives the same bits.  An output may be one of the call's inputs of the same type, shape and leading dimension (in place); any other overlap
- * is not allowed.  NaN and Inf go through the formulas.
+ * begin relative to 16 bytes, for column sums on whether an output lies over an input) and on nothing else, so the same call
+ * gives the same bits.  An output may be one of the call's inputs of the same type, shape and leading dimension (in place); any
+ * other overlap is not allowed.  NaN and Inf go through the formulas.
  */
 
 /*
@@ -403,8 +404,8 @@ size_t tmask_layer_norm_workspace_bytes(int64_t rows, int64_t cols);         /* 
  *     TMASK_GELU_ERF   y = u / 2 * (1 + erf(u / sqrt 2))
  *     TMASK_GELU_TANH  y = u / 2 * (1 + tanh(sqrt(2 / pi) * (u + 0.044715 u^3)))
  * and its gradients: dx = dy * dy/du, dbias (nullable, cols elements of param_dt) = sum_rows dx, from the same x and bias.
- * Finite u give finite results, however large, and u = +Inf gives y = +Inf.  The workspace (256-byte aligned, tmask_bias_gelu_workspace_bytes(rows, cols)) is
- * needed if dbias is asked for.
+ * Finite u give finite results, however large, and u = +Inf gives y = +Inf.  The workspace (256-byte aligned,
+ * tmask_bias_gelu_workspace_bytes(rows, cols)) is needed if dbias is asked for.
  */
 typedef enum { TMASK_GELU_ERF = 0, TMASK_GELU_TANH = 1 } tmask_gelu_form;
 

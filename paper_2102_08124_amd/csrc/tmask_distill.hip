@@ -337,7 +337,8 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
             const uint32_t c = threadIdx.x + (uint32_t)(i * T);
             raw[i / G][i % G] = no_chunk<DT>();
             if (c < row.full)
-                raw[i / G][i % G] = load_whole<DT, true>((const unsigned char *)a.logits + (z0 + row.head) * kSize<DT> + (size_t)(i * T) * 16u, threadIdx.x * 16u);
+                raw[i / G][i % G] = load_whole<DT, true>((const unsigned char *)a.logits + (z0 + row.head) * kSize<DT> + (size_t)(i * T) * 16u,
+                                                         threadIdx.x * 16u);
         }
         float t_max = -INFINITY;
         if (a.k) {
@@ -436,7 +437,8 @@ __device__ __forceinline__ void fetch(const DistillArgs &a, const Part &p, uint3
         const uint32_t c = c0 + threadIdx.x + (uint32_t)i * kSlice;
         raw[i] = no_chunk<DT>();
         if (c < p.end)
-            raw[i] = load_whole<DT, STREAM>((const unsigned char *)a.logits + (p.r * a.ld_logits + p.row.head) * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u);
+            raw[i] = load_whole<DT, STREAM>((const unsigned char *)a.logits + (p.r * a.ld_logits + p.row.head) * kSize<DT> +
+                                                (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u);
     }
 }
 
@@ -580,7 +582,8 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
                 for (int i = 0; i < kAhead; i++) {
                     const uint32_t c = c0 + threadIdx.x + (uint32_t)i * kSlice;
                     if (c < p.end)
-                        store_whole<DT, true>((unsigned char *)a.dlogits + (d0 + p.row.head) * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u, threadIdx.x * 16u, taken(raw[i]));
+                        store_whole<DT, true>((unsigned char *)a.dlogits + (d0 + p.row.head) * kSize<DT> + (size_t)(c0 + (uint32_t)i * kSlice) * 16u,
+                                              threadIdx.x * 16u, taken(raw[i]));
                 }
                 c0 += kAhead * kSlice;
                 if (c0 < p.end)

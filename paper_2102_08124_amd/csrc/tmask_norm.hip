@@ -331,13 +331,12 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormArgs 
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Its gradients, with rows held the same way.  A workgroup, one on a compute unit, goes through every strips-th group of rows and (unless the
-// batch is short: see norm_grad_columns) keeps
+// Its gradients, with rows held the same way.  A workgroup, one on a compute unit, goes through every strips-th group of rows and keeps
 // the sums over them of dy h and dy in registers, a column in the same lane all the time; at its end the lanes and wavefronts that share
-// a column add up in LDS, and the strips' sums are added up by columns_kernel.  Rows are loaded one ahead.  Bound by memory where
-// rows are many (8192 x 1024 bf16 with dtotal: 13.5 us and 2 for the sums, 4.4 TB/s of what has to be moved; 30000 x 1024 49 us, 5.0), by the rounds'
-// latencies where they are few (1003 x 2051 fp32 11.6 us).  Twice the strips with half the threads move twice the sums
-// (1000 x 4096 bf16: 22 us, like this 13).
+// a column add up in LDS, and the strips' sums are added up by columns_kernel.  Rows are loaded one ahead.  A short batch needs one launch:
+// see norm_grad_columns.  Bound by memory where rows are many (8192 x 1024 bf16 with dtotal: 13.5 us and 2 for the sums, 4.4 TB/s of what
+// has to be moved; 30000 x 1024 49 us, 5.0), by the rounds' latencies where they are few (1003 x 2051 fp32 10.5 us).  Twice the strips with
+// half the threads move twice the sums (1000 x 4096 bf16, in two launches: 22 us, like this 13).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kGradThreads = 1024;
 constexpr uint32_t kGradStrips = 256;
@@ -914,8 +913,8 @@ static const NormShape kNormShapes[] = {NORM_SHAPE(8, 8), NORM_SHAPE(16, 8), NOR
     {LANES * E, kGradThreads / LANES, {apart_lanes<kF32>(LANES * E), apart_lanes<kBF16>(LANES * E)},                              \
      {norm_grad_kernel<kF32, LANES, E>, norm_grad_kernel<kBF16, LANES, E>},                                                       \
      {norm_short_grad_kernel<kF32, LANES, E>, norm_short_grad_kernel<kBF16, LANES, E>}}
-static const NormGradShape kNormGradShapes[] = {GRAD_SHAPE(8, 8), GRAD_SHAPE(16, 8), GRAD_SHAPE(32, 8), GRAD_SHAPE(64, 8), GRAD_SHAPE(128, 8), GRAD_SHAPE(256, 8), GRAD_SHAPE(512, 8),
-                                                GRAD_SHAPE(1024, 8), GRAD_SHAPE(1024, 16)};
+static const NormGradShape kNormGradShapes[] = {GRAD_SHAPE(8, 8), GRAD_SHAPE(16, 8), GRAD_SHAPE(32, 8), GRAD_SHAPE(64, 8), GRAD_SHAPE(128, 8),
+                                                GRAD_SHAPE(256, 8), GRAD_SHAPE(512, 8), GRAD_SHAPE(1024, 8), GRAD_SHAPE(1024, 16)};
 #undef GRAD_SHAPE
 
 // the narrowest that holds the row, none for rows that no workgroup holds
