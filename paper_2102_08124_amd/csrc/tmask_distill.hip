@@ -59,7 +59,9 @@ static size_t list_bytes(uint32_t k, uint32_t hash_shift) { return 4u * (4u + 3u
 // exp(x / T) for x <= 0
 __device__ __forceinline__ float exp_of(const DistillArgs &a, float x) { return __builtin_amdgcn_exp2f(x * a.per_t2); }
 
-constexpr int kEntries = 4;               // that a thread reads at a time
+// entries that a thread of T reads at a time: all there can be, or four
+template <uint32_t T>
+constexpr int kEntries = T * 4u > kMaxEntries ? (int)(kMaxEntries / T) : 4;
 
 // Entry j of row r as it lies in memory: nothing is computed from it here, so that a thread's loads are all in flight at once.
 struct Entry {
@@ -111,41 +113,64 @@ __device__ __forceinline__ void enter(const DistillArgs &a, const List &l, int32
     }
 }
 
-// Reads row r's list into LDS; as_logit(logit(at, j)): the student's logit of entry j, loaded and made fp32; noted(at): whether
-// repeats of that column matter.  The result is the thread's largest logit of an entry (+Inf for NaN), -Inf if it has none.
-template <uint32_t T, typename Logit, typename AsLogit, typename Noted>
-__device__ __forceinline__ float read_list(const DistillArgs &a, uint32_t r, const List &l, Logit logit, AsLogit as_logit, Noted noted)
+template <uint32_t T>
+struct Entries {
+    Entry e[kEntries<T>];
+};
+
+// the thread's entries from j0 on
+template <uint32_t T>
+__device__ __forceinline__ Entries<T> fetch_entries(const DistillArgs &a, uint32_t r, uint32_t j0)
+{
+    Entries<T> some;
+#pragma unroll
+    for (int i = 0; i < kEntries<T>; i++)
+        if (j0 + (uint32_t)i * T < a.k)
+            some.e[i] = entry_at(a, r, j0 + (uint32_t)i * T);
+    return some;
+}
+
+// Reads row r's list into LDS; `first`: the thread's first entries; logit(at, j): the student's logit of entry j, loaded, and
+// as_logit made fp32; noted(at): whether repeats of that column matter; meanwhile(): what else there is to do while the logits arrive.
+// Loads come back in their order, so entries are asked for before the row, their logits behind it.  The result is the
+// thread's largest logit of an entry (+Inf for NaN), -Inf if it has none.
+template <uint32_t T, typename Logit, typename AsLogit, typename Noted, typename Meanwhile>
+__device__ __forceinline__ float read_list(const DistillArgs &a, uint32_t r, const List &l, const Entries<T> &first, Logit logit, AsLogit as_logit,
+                                           Noted noted, Meanwhile meanwhile)
 {
     float t_max = -INFINITY;
-    for (uint32_t j0 = threadIdx.x; j0 < a.k; j0 += kEntries * T) {
-        Entry e[kEntries];
-        int32_t at[kEntries];
-        decltype(logit(0, 0u)) z[kEntries];
+    auto take = [&](uint32_t j0, const Entries<T> &some, auto &&then) {
+        decltype(logit(0, 0u)) z[kEntries<T>];
+        int32_t at[kEntries<T>];
 #pragma unroll
-        for (int i = 0; i < kEntries; i++)
-            if (j0 + (uint32_t)i * T < a.k)
-                e[i] = entry_at(a, r, j0 + (uint32_t)i * T);
-#pragma unroll
-        for (int i = 0; i < kEntries; i++) {
-            at[i] = j0 + (uint32_t)i * T < a.k ? column_of(a, e[i]) : -1;
+        for (int i = 0; i < kEntries<T>; i++) {
+            at[i] = j0 + (uint32_t)i * T < a.k ? column_of(a, some.e[i]) : -1;
             if (at[i] >= 0)
                 z[i] = logit(at[i], j0 + (uint32_t)i * T);
         }
 #pragma unroll
-        for (int i = 0; i < kEntries; i++) {
+        for (int i = 0; i < kEntries<T>; i++) {
             const uint32_t j = j0 + (uint32_t)i * T;
             if (j < a.k)
                 l.at[j] = at[i];
             if (at[i] >= 0) {
-                const float t = logit_of(a, e[i]);
+                const float t = logit_of(a, some.e[i]);
                 l.t[j] = t;
-                l.z[j] = as_logit(z[i]);
                 t_max = fmaxf(t_max, t != t ? INFINITY : t);
                 if (noted(at[i]))
                     enter(a, l, at[i]);
             }
         }
-    }
+        then();
+#pragma unroll
+        for (int i = 0; i < kEntries<T>; i++)
+            if (at[i] >= 0)
+                l.z[j0 + (uint32_t)i * T] = as_logit(z[i]);
+    };
+    take(threadIdx.x, first, meanwhile);
+    if constexpr (T * kEntries<T> < kMaxEntries)
+        for (uint32_t j0 = threadIdx.x + kEntries<T> * T; j0 < a.k; j0 += kEntries<T> * T)
+            take(j0, fetch_entries<T>(a, r, j0), [] {});
     return t_max;
 }
 
@@ -329,6 +354,7 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
         const size_t z0 = r * a.ld_logits;
         const RowShape row = shape_of<DT>(a, r);
         const Edge edge = edge_of(a, row.head, row.tail);
+        const Entries<T> first = fetch_entries<T>(a, r, threadIdx.x);
         const uint32_t edge_bits = edge.there ? load_bits<DT>(a.logits, z0 + edge.at) : 0u;
         u32x4 raw[P / G][G];
         const float g = a.dlogits ? (a.row_weight ? a.row_weight[r] : 1.f) * a.temperature : 0.f;
@@ -340,19 +366,21 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
                 raw[i / G][i % G] = load_whole<DT, true>((const unsigned char *)a.logits + (z0 + row.head) * kSize<DT> + (size_t)(i * T) * 16u,
                                                          threadIdx.x * 16u);
         }
-        float t_max = -INFINITY;
         if (a.k) {
             clear_table<T>(a, list);
             __syncthreads();
-            t_max = read_list<T>(a, r, list, [&](int32_t at, uint32_t) { return load_bits<DT>(a.logits, z0 + (uint32_t)at); }, from_bits<DT>,
-                                 [&](int32_t) { return a.dlogits != nullptr; });
         }
         const float single = from_bits<DT>(edge_bits);
-        Running run = start(a, edge, single);
+        Running run;
+        float t_max = read_list<T>(a, r, list, first, [&](int32_t at, uint32_t) { return load_bits<DT>(a.logits, z0 + (uint32_t)at); }, from_bits<DT>,
+                                   [&](int32_t) { return a.dlogits != nullptr; },
+                                   [&] {
+                                       run = start(a, edge, single);
 #pragma unroll
-        for (int i = 0; i < P / G; i++)
-            if ((uint32_t)(i * G * T) < row.full)
-                add_chunks<DT, G>(a, run, raw[i]);
+                                       for (int i = 0; i < P / G; i++)
+                                           if ((uint32_t)(i * G * T) < row.full)
+                                               add_chunks<DT, G>(a, run, raw[i]);
+                                   });
         float z_max = run.max;
         group_reduce<Max, Max, W>(t_max, z_max, red);
         float t_sum = entries_sum<T>(a, list, t_max), z_sum = relative(a, run, z_max);
@@ -442,8 +470,21 @@ __device__ __forceinline__ void fetch(const DistillArgs &a, const Part &p, uint3
     }
 }
 
+// adds up the chunks c0 ... that the workgroup fetched: by four of a thread, and not those behind the part
 template <int DT>
-__global__ void __launch_bounds__(kSlice) distill_part_kernel(const DistillArgs a)
+__device__ __forceinline__ void add_fetched(const DistillArgs &a, const Part &p, uint32_t c0, Running &run, u32x4 (&raw)[kAhead])
+{
+    constexpr int G = 4;
+#pragma unroll
+    for (int i = 0; i < kAhead; i += G)
+        if (c0 + (uint32_t)i * kSlice < p.end) {
+            u32x4 some[G] = {raw[i], raw[i + 1], raw[i + 2], raw[i + 3]};
+            add_chunks<DT, G>(a, run, some);
+        }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kSlice, 8) distill_part_kernel(const DistillArgs a)
 {
     constexpr int W = kSlice / 64;
     __shared__ float red[4 * W];
@@ -454,7 +495,7 @@ __global__ void __launch_bounds__(kSlice) distill_part_kernel(const DistillArgs 
         for (uint32_t c0 = p.begin; c0 < p.end; c0 += kAhead * kSlice) {
             u32x4 raw[kAhead];
             fetch<DT, false>(a, p, c0, raw);
-            add_chunks<DT, kAhead>(a, run, raw);
+            add_fetched<DT>(a, p, c0, run, raw);
         }
         float all = run.max, unused = 0.f;
         group_reduce<Max, Max, W>(all, unused, red);
@@ -475,7 +516,7 @@ __global__ void __launch_bounds__(kSlice) distill_part_kernel(const DistillArgs 
     }
 }
 
-// The loss alone of rows that are added up without being held, so that a compute unit has eight workgroups' loads in flight.
+// The loss alone of rows that are added up without being held, so that a compute unit has seven workgroups' loads in flight.
 template <int DT>
 __global__ void __launch_bounds__(kSlice) distill_loss_kernel(const DistillArgs a)
 {
@@ -486,16 +527,19 @@ __global__ void __launch_bounds__(kSlice) distill_loss_kernel(const DistillArgs 
     for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Part p = part_of<DT>(a, r);                                       // the whole row
         const size_t z0 = r * a.ld_logits;
+        const Entries<kSlice> first = fetch_entries<kSlice>(a, r, threadIdx.x);
         const uint32_t edge_bits = p.edge.there ? load_bits<DT>(a.logits, z0 + p.edge.at) : 0u;
-        float t_max = a.k ? read_list<kSlice>(a, r, list, [&](int32_t at, uint32_t) { return load_bits<DT>(a.logits, z0 + (uint32_t)at); },
-                                                 from_bits<DT>, [](int32_t) { return false; })
-                             : -INFINITY;
-        Running run = start(a, p.edge, from_bits<DT>(edge_bits));
-        for (uint32_t c0 = p.begin; c0 < p.end; c0 += kAhead * kSlice) {
-            u32x4 raw[kAhead];
-            fetch<DT, true>(a, p, c0, raw);
-            add_chunks<DT, kAhead>(a, run, raw);
-        }
+        Running run;
+        float t_max = read_list<kSlice>(a, r, list, first, [&](int32_t at, uint32_t) { return load_bits<DT>(a.logits, z0 + (uint32_t)at); }, from_bits<DT>,
+                                        [](int32_t) { return false; },
+                                        [&] {
+                                            run = start(a, p.edge, from_bits<DT>(edge_bits));
+                                            for (uint32_t c0 = p.begin; c0 < p.end; c0 += kAhead * kSlice) {
+                                                u32x4 raw[kAhead];
+                                                fetch<DT, true>(a, p, c0, raw);
+                                                add_fetched<DT>(a, p, c0, run, raw);
+                                            }
+                                        });
         float z_max = run.max;
         group_reduce<Max, Max, W>(t_max, z_max, red);
         float t_sum = entries_sum<kSlice>(a, list, t_max), z_sum = relative(a, run, z_max);
@@ -524,6 +568,7 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
         if (JOIN && !a.dlogits && p.part)                                       // the loss alone is joined by one workgroup a row
             continue;
         const size_t z0 = p.r * a.ld_logits;
+        const Entries<kSlice> first = fetch_entries<kSlice>(a, p.r, threadIdx.x);
         const uint32_t edge_bits = a.dlogits && p.edge.there ? load_bits<DT>(a.logits, z0 + p.edge.at) : 0u;
         u32x4 raw[kAhead];
         if (a.dlogits)
@@ -549,7 +594,7 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
                 clear_table<kSlice>(a, list);
                 __syncthreads();
             }
-            t_max = read_list<kSlice>(a, p.r, list,
+            t_max = read_list<kSlice>(a, p.r, list, first,
                                       [&](int32_t at, uint32_t j) {
                                           if constexpr (JOIN)
                                               return __float_as_uint(a.list_logits[(size_t)p.r * a.k + j]);
@@ -557,7 +602,7 @@ __global__ void __launch_bounds__(kSlice) distill_slice_kernel(const DistillArgs
                                               return load_bits<DT>(a.logits, z0 + (uint32_t)(in_part(p, at) ? at : 0));
                                       },
                                       [](uint32_t bits) { return JOIN ? __uint_as_float(bits) : from_bits<DT>(bits); },
-                                      [&](int32_t at) { return a.dlogits && in_part(p, at); });
+                                      [&](int32_t at) { return a.dlogits && in_part(p, at); }, [] {});
         }
         group_reduce<Max, Max, W>(t_max, unused, red);
         t_sum = entries_sum<kSlice>(a, list, t_max);
@@ -619,10 +664,12 @@ struct RowKernel {
 // overlaps, and a row is done soonest by many threads (64 rows of 8000 bf16: 64 threads with 16 chunks 10.1 us, 1024 with 4 6.8).  In between
 // the chip takes so many wavefronts of a row at once: 4000 rows of 2304 fp32 by 256 threads 24.4 us, by 64 17.7, but 400 rows 6.6 and 7.4; 2000 of
 // 9000 bf16 by 256 threads 23.1, by 128 20.1, 400 of 10000 9.2 and 10.7; 300 of 2304 bf16 by 64 threads 7.1, by 256 6.6, 800 7.5 and 8.0.
+// Long rows: two workgroups on a compute unit, as long as their registers last (4000 rows of 80000 bf16 by 256 threads with 40 chunks 243 us, by 512 with
+// 32, alone on their unit, 294; with 44, which spill, 329), then one of many wavefronts (of 120000, 1024 threads with 16 chunks 403, 512 with 32 426).
 // The first that holds the row and is for so many.
 static const RowKernel kManyRows[] = {ROW_KERNEL(64, 4, 0), ROW_KERNEL(64, 8, 640), ROW_KERNEL(64, 12, 1536), ROW_KERNEL(128, 8, 1536), ROW_KERNEL(256, 4, 0),
-                                      ROW_KERNEL(128, 12, 640), ROW_KERNEL(256, 8, 0), ROW_KERNEL(256, 16, 0), ROW_KERNEL(512, 16, 0), ROW_KERNEL(512, 32, 0),
-                                      ROW_KERNEL(512, 44, 0)};
+                                      ROW_KERNEL(128, 12, 640), ROW_KERNEL(256, 8, 0), ROW_KERNEL(256, 16, 0), ROW_KERNEL(512, 16, 0), ROW_KERNEL(256, 40, 0),
+                                      ROW_KERNEL(1024, 12, 0), ROW_KERNEL(1024, 16, 0), ROW_KERNEL(512, 44, 0)};
 static const RowKernel kFewRows[] = {ROW_KERNEL(64, 4, 0), ROW_KERNEL(256, 4, 0), ROW_KERNEL(1024, 4, 0), ROW_KERNEL(1024, 8, 0)};
 constexpr int64_t kFew = 256;
 // Without a gradient longer rows need not be held (3000 rows of 64000 fp32: 148 us held, 117 not; of 4000, 1000 chunks, 14.7 both).

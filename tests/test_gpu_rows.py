@@ -417,7 +417,8 @@ def test_distill_rows_lists_and_types(rows, vocab, k, dt, tdt, bits, T):
 # around the lengths at which a row goes to another workgroup, to parts, or (without a gradient) through one that does not hold it
 @pytest.mark.parametrize("rows,vocab", [(70, 1026), (70, 4098), (70, 16390), (70, 32763), (70, 32779), (256, 40000), (257, 1021), (257, 1029), (257, 2050), (257, 4095),
                                         (257, 4105), (257, 8200), (257, 16390), (257, 32775), (257, 65530), (257, 65545), (257, 90112), (257, 90117),
-                                        (641, 2045), (641, 5000), (1537, 2050), (1537, 3070), (1537, 3080), (1537, 4099), (1537, 6150)])
+                                        (641, 2045), (641, 5000), (1537, 2050), (1537, 3070), (1537, 3080), (1537, 4099), (1537, 6150),
+                                        (257, 40965), (257, 49160)])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_distill_rows_of_every_kernel(rows, vocab, dt):
     vocab = vocab if dt == "f32" else 2 * vocab - 1              # twice the elements to a chunk
