@@ -336,15 +336,17 @@ __device__ __forceinline__ void write_row(const DistillArgs &a, uint32_t r, cons
 
 // ---------------------------------------------------------------------------------------------------------------------
 // A row in the registers of one workgroup: T threads with P chunks each.  The logits are read once, added up as they arrive, and the
-// gradient is taken from the registers.  Bound by memory: 4096 rows of 32000 bf16, loss and gradient, 104 us (524 MB, 5.0 TB/s,
+// gradient is taken from the registers.  Bound by memory: 4096 rows of 32000 bf16, loss and gradient, 102 us (524 MB, 5.1 TB/s,
 // a device copy's rate; the vector ALU is busy for half of that time).  Logits and gradient pass with streaming loads and stores (with plain
 // ones 119 us).
 //
 // The gradient's columns that the list names are written again, with what the teacher takes from them, when the rest has been
 // written: k of the vocabulary's columns, and the barrier between orders the two (the counters see 4 % more bytes written).
 // ---------------------------------------------------------------------------------------------------------------------
-template <int DT, int T, int P>
-__global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
+// LONGER: what the workgroup does not hold is read twice, the second time from the memory-side cache, which has room for that of a row for
+// each compute unit (4000 rows of 120000 fp32 767 us, 5.0 TB/s; in parts, with two passes over all rows, 1011).
+template <int DT, int T, int P, bool LONGER>
+__device__ __forceinline__ void distill_row(const DistillArgs a)
 {
     constexpr int W = T / 64, G = 4;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -366,6 +368,15 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
                 raw[i / G][i % G] = load_whole<DT, true>((const unsigned char *)a.logits + (z0 + row.head) * kSize<DT> + (size_t)(i * T) * 16u,
                                                          threadIdx.x * 16u);
         }
+        auto behind = [&](uint32_t c0, u32x4 (&some)[G]) {                      // chunks that are not held
+#pragma unroll
+            for (int i = 0; i < G; i++) {
+                some[i] = no_chunk<DT>();
+                if (c0 + threadIdx.x + (uint32_t)(i * T) < row.full)
+                    some[i] = load_whole<DT>((const unsigned char *)a.logits + (z0 + row.head) * kSize<DT> + (size_t)(c0 + (uint32_t)(i * T)) * 16u,
+                                             threadIdx.x * 16u);
+            }
+        };
         if (a.k) {
             clear_table<T>(a, list);
             __syncthreads();
@@ -380,6 +391,12 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
                                        for (int i = 0; i < P / G; i++)
                                            if ((uint32_t)(i * G * T) < row.full)
                                                add_chunks<DT, G>(a, run, raw[i]);
+                                       if constexpr (LONGER)
+                                           for (uint32_t c0 = T * P; c0 < row.full; c0 += G * T) {
+                                               u32x4 some[G];
+                                               behind(c0, some);
+                                               add_chunks<DT, G>(a, run, some);
+                                           }
                                    });
         float z_max = run.max;
         group_reduce<Max, Max, W>(t_max, z_max, red);
@@ -403,6 +420,16 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
                     store_whole<DT, true>((unsigned char *)a.dlogits + (d0 + row.head) * kSize<DT> + (size_t)(i * T) * 16u, me * 16u,
                                           none ? u32x4{0u, 0u, 0u, 0u} : pull<DT>(a, raw[i / G][i % G], z_max, g_q));
             }
+            if constexpr (LONGER)
+                for (uint32_t c0 = T * P; c0 < row.full; c0 += G * T) {
+                    u32x4 some[G];
+                    behind(c0, some);
+#pragma unroll
+                    for (int i = 0; i < G; i++)
+                        if (c0 + me + (uint32_t)(i * T) < row.full)
+                            store_whole<DT, true>((unsigned char *)a.dlogits + (d0 + row.head) * kSize<DT> + (size_t)(c0 + (uint32_t)(i * T)) * 16u, me * 16u,
+                                                  none ? u32x4{0u, 0u, 0u, 0u} : pull<DT>(a, some[i], z_max, g_q));
+                }
             if (edge.there)
                 store_one<DT>(a.dlogits, d0 + edge.at, none ? 0.f : exp_of(a, single - z_max) * g_q);
         }
@@ -422,8 +449,22 @@ __global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
     }
 }
 
+template <int DT, int T, int P>
+__global__ void __launch_bounds__(T) distill_row_kernel(const DistillArgs a)
+{
+    distill_row<DT, T, P, false>(a);
+}
+
+constexpr int kLong = 1024;
+
+template <int DT>
+__global__ void __launch_bounds__(kLong) distill_long_kernel(const DistillArgs a)
+{
+    distill_row<DT, kLong, 12, true>(a);
+}
+
 // ---------------------------------------------------------------------------------------------------------------------
-// Few rows, or rows that no workgroup holds: parts of rows.  The first launch takes the maximum and the sum of each part and the
+// Few long rows: parts of rows.  The first launch takes the maximum and the sum of each part and the
 // student's logits of the entries in it; the second joins them and does the rest, part by part, from logits that the caches may
 // still hold.  48 rows of 131072 fp32, loss and gradient: 7 and 10 us (25 MB read, then 25 read from the caches and 25 written).
 // A gradient alone has its statistics and needs the second launch only: 1003 rows of 50021 bf16 43 us (4.6 TB/s).
@@ -665,17 +706,19 @@ struct RowKernel {
 // the chip takes so many wavefronts of a row at once: 4000 rows of 2304 fp32 by 256 threads 24.4 us, by 64 17.7, but 400 rows 6.6 and 7.4; 2000 of
 // 9000 bf16 by 256 threads 23.1, by 128 20.1, 400 of 10000 9.2 and 10.7; 300 of 2304 bf16 by 64 threads 7.1, by 256 6.6, 800 7.5 and 8.0.
 // Long rows: two workgroups on a compute unit, as long as their registers last (4000 rows of 80000 bf16 by 256 threads with 40 chunks 243 us, by 512 with
-// 32, alone on their unit, 294; with 44, which spill, 329), then one of many wavefronts (of 120000, 1024 threads with 16 chunks 403, 512 with 32 426).
+// 32, alone on their unit, 294; with 44, which spill, 329), then one of many wavefronts (of 120000, 1024 threads with 16 chunks 403, 512 with 32 426; of
+// 80000 fp32, 512 with 44 chunks 482, by distill_long_kernel 472).
 // The first that holds the row and is for so many.
 static const RowKernel kManyRows[] = {ROW_KERNEL(64, 4, 0), ROW_KERNEL(64, 8, 640), ROW_KERNEL(64, 12, 1536), ROW_KERNEL(128, 8, 1536), ROW_KERNEL(256, 4, 0),
                                       ROW_KERNEL(128, 12, 640), ROW_KERNEL(256, 8, 0), ROW_KERNEL(256, 16, 0), ROW_KERNEL(512, 16, 0), ROW_KERNEL(256, 40, 0),
-                                      ROW_KERNEL(1024, 12, 0), ROW_KERNEL(1024, 16, 0), ROW_KERNEL(512, 44, 0)};
+                                      ROW_KERNEL(1024, 12, 0), ROW_KERNEL(1024, 16, 0)};
 static const RowKernel kFewRows[] = {ROW_KERNEL(64, 4, 0), ROW_KERNEL(256, 4, 0), ROW_KERNEL(1024, 4, 0), ROW_KERNEL(1024, 8, 0)};
 constexpr int64_t kFew = 256;
+constexpr uint32_t kFewHeld = 1024 * 8;
 // Without a gradient longer rows need not be held (3000 rows of 64000 fp32: 148 us held, 117 not; of 4000, 1000 chunks, 14.7 both).
 constexpr uint32_t kLossHeld = 1024;
 #undef ROW_KERNEL
-constexpr uint32_t kHeld = 512 * 44;
+constexpr uint32_t kHeld = 1024 * 16;      // longer rows: distill_long_kernel
 
 // How a call is cut: parts = 0 is a row per workgroup.
 struct Cut {
@@ -698,12 +741,13 @@ static Cut cut_rows(int64_t rows, uint32_t chunks, uint32_t least, uint32_t most
 
 static uint32_t chunks_of(int64_t vocab, tmask_dtype dt) { return (uint32_t)(vocab / (dt == TMASK_F32 ? 4 : 8)); }   // of a row at most
 
-static Cut cut_loss(int64_t rows, int64_t vocab, tmask_dtype dt, bool alone)
+static Cut cut_loss(int64_t rows, int64_t vocab, tmask_dtype dt)
 {
     const uint32_t chunks = chunks_of(vocab, dt);
     // A second launch costs 3 us; a row in one workgroup longer, the longer it is and the fewer compute units have one (us, row / parts:
-    // 16 rows of 32000 bf16 8.4 / 10.0, of 64000 11.9 / 10.1; 64 rows of 64000 12.6 / 15.4, of 131072 22.8 / 16.5; 256 rows of 131072 34 both).
-    if (chunks <= 4096 || rows >= (chunks <= 8192 ? 64 : chunks <= kHeld || alone ? kFew + 1 : INT64_MAX))
+    // 16 rows of 32000 bf16 8.4 / 10.0, of 64000 11.9 / 10.1; 64 rows of 64000 12.6 / 15.4, of 131072 21.1 / 15.0; 128 of 89000 17.1 / 18.1, of
+    // 131072 fp32 32.1 / 35.6; 256 57.7 / 69.4).
+    if (chunks <= 4096 || rows >= (chunks <= kFewHeld ? 64 : 128))
         return {0, 0};
     return cut_rows(rows, chunks, 512, kAhead * kSlice);
 }
@@ -756,7 +800,7 @@ extern "C" size_t tmask_distill_workspace_bytes(int64_t rows, int64_t vocab)
         return 0;
     size_t most = 0;
     for (const tmask_dtype dt : {TMASK_F32, TMASK_BF16}) {
-        const size_t parts = cut_loss(rows, vocab, dt, false).parts;
+        const size_t parts = cut_loss(rows, vocab, dt).parts;
         const size_t need = parts ? (size_t)rows * (2u * parts + kMaxEntries) * 4u : 0;
         most = need > most ? need : most;
     }
@@ -774,7 +818,7 @@ extern "C" int tmask_distill(const tmask_distill_desc *desc, tmask_dtype dt, tma
     TMASK_TRY(check_vector("row_max", desc->row_max, 4, desc->row_sum != nullptr));
     TMASK_TRY(check_vector("row_sum", desc->row_sum, 4, desc->row_max != nullptr));
     hipStream_t stream = (hipStream_t)hip_stream;
-    const Cut cut = cut_loss(desc->rows, desc->vocab, dt, !a.dlogits);
+    const Cut cut = cut_loss(desc->rows, desc->vocab, dt);
     const size_t list = list_bytes(a.k, a.hash_shift);
     const bool bf16 = dt == TMASK_BF16;
     if (cut.parts == 0 && !a.dlogits && desc->rows > kFew && chunks_of(desc->vocab, dt) > kLossHeld) {
@@ -783,10 +827,16 @@ extern "C" int tmask_distill(const tmask_distill_desc *desc, tmask_dtype dt, tma
         hipLaunchKernelGGL(bf16 ? distill_loss_kernel<kBF16> : distill_loss_kernel<kF32>, dim3(grid_of(a.rows)), dim3(kSlice), 20 * (kSlice / 64) + list,
                            stream, a);
     } else if (cut.parts == 0) {
-        const RowKernel *k = desc->rows <= kFew ? kFewRows : kManyRows;
-        while (k->chunks < chunks_of(desc->vocab, dt) || desc->rows <= k->above)
-            k++;
-        hipLaunchKernelGGL(k->kernel[bf16], dim3(grid_of(a.rows)), dim3(k->threads), 20 * (k->threads / 64) + list, stream, a);
+        const uint32_t chunks = chunks_of(desc->vocab, dt);
+        if (chunks > kHeld) {
+            hipLaunchKernelGGL(bf16 ? distill_long_kernel<kBF16> : distill_long_kernel<kF32>, dim3(grid_of(a.rows)), dim3(kLong), 20 * (kLong / 64) + list,
+                               stream, a);
+        } else {
+            const RowKernel *k = desc->rows <= kFew && chunks <= kFewHeld ? kFewRows : kManyRows;
+            while (k->chunks < chunks || desc->rows <= k->above)
+                k++;
+            hipLaunchKernelGGL(k->kernel[bf16], dim3(grid_of(a.rows)), dim3(k->threads), 20 * (k->threads / 64) + list, stream, a);
+        }
     } else {
         TMASK_TRY(check_workspace(workspace, workspace_bytes, tmask_distill_workspace_bytes(desc->rows, desc->vocab)));
         a.parts = cut.parts;

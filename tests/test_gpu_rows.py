@@ -418,7 +418,7 @@ def test_distill_rows_lists_and_types(rows, vocab, k, dt, tdt, bits, T):
 @pytest.mark.parametrize("rows,vocab", [(70, 1026), (70, 4098), (70, 16390), (70, 32763), (70, 32779), (256, 40000), (257, 1021), (257, 1029), (257, 2050), (257, 4095),
                                         (257, 4105), (257, 8200), (257, 16390), (257, 32775), (257, 65530), (257, 65545), (257, 90112), (257, 90117),
                                         (641, 2045), (641, 5000), (1537, 2050), (1537, 3070), (1537, 3080), (1537, 4099), (1537, 6150),
-                                        (257, 40965), (257, 49160)])
+                                        (257, 40965), (257, 49160), (257, 70001), (127, 33000), (128, 33000), (128, 131075), (130, 65541)])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_distill_rows_of_every_kernel(rows, vocab, dt):
     vocab = vocab if dt == "f32" else 2 * vocab - 1              # twice the elements to a chunk
@@ -515,7 +515,7 @@ def test_distill_keeps_bad_rows_to_themselves(vocab, bad):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,vocab", [(3, 100), (300, 3000), (3, 100000)])
+@pytest.mark.parametrize("rows,vocab", [(3, 100), (300, 3000), (3, 100000), (130, 140000)])
 def test_distill_in_place(rows, vocab, dt):
     m = Maker(4)
     z = m.normal((rows, vocab), TYPES[dt], 3.0)
@@ -527,6 +527,26 @@ def test_distill_in_place(rows, vocab, dt):
     tm.tmask_distill_backward(z2, teacher, index, 1.0, top, total, z2)
     torch.cuda.synchronize()
     assert torch.equal(loss, loss1) and torch.equal(z1, dz) and torch.equal(z2, dz)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_distill_longest_rows_keep_to_themselves(dt):
+    m = Maker(16)
+    z = m.normal((130, 140001), TYPES[dt], 3.0)
+    teacher, index = lists(m, 130, 140001, 16, TYPES[dt], 64)
+    loss, dz, ws = torch.empty(130, device="cuda"), torch.empty_like(z), tm.alloc_distill_workspace(z)
+    tm.tmask_distill(z, teacher, index, 1.0, loss, dlogits=dz, workspace=ws)
+    torch.cuda.synchronize()
+    first, first_dz = loss.clone(), dz.clone()
+    z[5], z[7, 139999], z[9, 140000], z[11, :140000] = float("-inf"), float("nan"), float("inf"), float("-inf")
+    teacher[13] = float("-inf")
+    tm.tmask_distill(z, teacher, index, 1.0, loss, dlogits=dz, workspace=ws)
+    torch.cuda.synchronize()
+    others = [r for r in range(130) if r not in (5, 7, 9, 11, 13)]
+    assert torch.equal(loss[others], first[others]) and torch.equal(dz[others], first_dz[others])
+    assert not loss[[5, 7, 9]].isfinite().any() and dz[7].isnan().all()
+    assert loss[13] == 0 and not dz[13].any()
+    assert loss[11] == float("inf") and dz[11, 140000] == 1.0                   # one column left, and not one of the list's
 
 
 def far(m, rows, cols, dtype):
