@@ -200,8 +200,8 @@ struct Running {
 
 // G chunks more, at a price of one exponential for the sum so far.  The empty statement keeps the compiler from holding
 // the unpacked elements of a row, twice its registers, until the gradient.
-template <int DT, int G>
-__device__ __forceinline__ void add_chunks(const DistillArgs &a, Running &run, u32x4 (&raw)[G])
+template <int DT, int G, int ALL>
+__device__ __forceinline__ void add_chunks(const DistillArgs &a, Running &run, u32x4 (&raw)[ALL])
 {
     constexpr int N = kElems<DT>;
     float v[N], m = run.max, s = 0.f;
@@ -338,7 +338,8 @@ __device__ __forceinline__ void write_row(const DistillArgs &a, uint32_t r, cons
 // A row in the registers of one workgroup: T threads with P chunks each.  The logits are read once, added up as they arrive, and the
 // gradient is taken from the registers.  Bound by memory: 4096 rows of 32000 bf16, loss and gradient, 102 us (524 MB, 5.1 TB/s,
 // a device copy's rate; the vector ALU is busy for half of that time).  Logits and gradient pass with streaming loads and stores (with plain
-// ones 119 us).
+// ones 119 us); but the gradient of short rows, whose lines the list's columns soon touch again, with plain stores (8000 rows of 900 fp32 18.3 us,
+// streaming 19.6).
 //
 // The gradient's columns that the list names are written again, with what the teacher takes from them, when the rest has been
 // written: k of the vocabulary's columns, and the barrier between orders the two (the counters see 4 % more bytes written).
@@ -349,6 +350,7 @@ template <int DT, int T, int P, bool LONGER>
 __device__ __forceinline__ void distill_row(const DistillArgs a)
 {
     constexpr int W = T / 64, G = 4;
+    constexpr int kAtOnce = P <= 12 ? G / 2 : 0;                                // a group's second half only if the row has it: short rows' arithmetic counts
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     float *const red = (float *)lds;                                            // 2 x 2 W numbers, and W
     const List list = list_in(red + 5 * W, a);
@@ -389,8 +391,10 @@ __device__ __forceinline__ void distill_row(const DistillArgs a)
                                        run = start(a, edge, single);
 #pragma unroll
                                        for (int i = 0; i < P / G; i++)
-                                           if ((uint32_t)(i * G * T) < row.full)
+                                           if ((uint32_t)((i * G + kAtOnce) * T) < row.full)
                                                add_chunks<DT, G>(a, run, raw[i]);
+                                           else if (kAtOnce && (uint32_t)(i * G * T) < row.full)
+                                               add_chunks<DT, G / 2>(a, run, raw[i]);
                                        if constexpr (LONGER)
                                            for (uint32_t c0 = T * P; c0 < row.full; c0 += G * T) {
                                                u32x4 some[G];
@@ -417,7 +421,7 @@ __device__ __forceinline__ void distill_row(const DistillArgs a)
 #pragma unroll
             for (int i = 0; i < P; i++) {
                 if (me + (uint32_t)(i * T) < row.full)
-                    store_whole<DT, true>((unsigned char *)a.dlogits + (d0 + row.head) * kSize<DT> + (size_t)(i * T) * 16u, me * 16u,
+                    store_whole<DT, (T * P > 256)>((unsigned char *)a.dlogits + (d0 + row.head) * kSize<DT> + (size_t)(i * T) * 16u, me * 16u,
                                           none ? u32x4{0u, 0u, 0u, 0u} : pull<DT>(a, raw[i / G][i % G], z_max, g_q));
             }
             if constexpr (LONGER)
