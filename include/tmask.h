@@ -439,7 +439,8 @@ size_t tmask_bias_gelu_workspace_bytes(int64_t rows, int64_t cols);          /* 
  *     dlogits[r][v] = row_weight[r] * T * (q_v - sum of p_j over the entries with index(j) = v)
  * A row without an entry has loss 0 and gradient 0; a row whose weight is 0 (padding) has gradient 0 whatever its logits are.
  * An index that is given several times counts several times.  A masked logit (-Inf or the type's lowest value) has q = 0: an entry
- * for which the student has q = 0 by -Inf makes the loss +Inf, the gradient stays finite.  Logits that hold NaN or +Inf, or nothing but -Inf, make
+ * for which the student has q = 0 by -Inf makes the loss +Inf, the gradient stays finite; by the lowest value the loss is as large as the
+ * formula has it.  An entry whose p is below the least normal number of fp32 adds nothing otherwise.  Logits that hold NaN or +Inf, or nothing but -Inf, make
  * the row's loss and gradient NaN.
  * row_max[r] = max_v z, row_sum[r] = sum_v exp((z_v - row_max) / T): nullable outputs, both or neither (q and the
  * gradient follow from them later; row_max ignores NaN).

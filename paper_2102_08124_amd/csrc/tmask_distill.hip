@@ -32,7 +32,7 @@ struct DistillArgs {
     uint32_t parts, part_chunks;
     uint32_t teacher_f32, index64;
     uint32_t hash_shift;
-    float temperature, per_t, per_t2;     // T, 1 / T, log2(e) / T
+    float temperature, per_t2;            // T, log2(e) / T
 };
 
 // A row's list in LDS, k numbers each: columns (-1: no entry), the teacher's logits (later: its probabilities), the student's logits.
@@ -291,18 +291,21 @@ __device__ __forceinline__ u32x4 pull(const DistillArgs &a, u32x4 raw, float z_m
     return pack<DT>(v);
 }
 
-// Turns the logits of a thread's entries into probabilities; the result is what they add to the loss, without T^2.
+// Turns the logits of a thread's entries into probabilities; the result is what they add to the loss, in units of T.  With logarithms times T
+// a logit of the type's lowest value stays a number where 1 / T of it is none.  An entry that has lost its probability adds nothing, unless
+// the student's logit is -Inf; so does p log p at p = 0.
 template <uint32_t T, bool LOSS = true>
 __device__ __forceinline__ float take_entries(const DistillArgs &a, const List &list, float t_max, float t_sum, float z_max, float z_sum)
 {
-    const float t_log = LOSS ? logf(t_sum) : 0.f, z_log = LOSS ? logf(z_sum) : 0.f, part = 1.f / t_sum;
+    const float t_log = LOSS ? a.temperature * logf(t_sum) : 0.f, z_log = LOSS ? a.temperature * logf(z_sum) : 0.f, part = 1.f / t_sum;
     float loss = 0.f;
     for (uint32_t j = threadIdx.x; j < a.k; j += T)
         if (list.at[j] >= 0) {
             const float t = list.t[j] - t_max, p = exp_of(a, t) * part;
             if constexpr (LOSS) {
-                const float log_q = (list.z[j] - z_max) * a.per_t - z_log;
-                loss += log_q == -INFINITY ? INFINITY : p * ((t * a.per_t - t_log) - log_q);
+                const float z = list.z[j], log_q = (z - z_max) - z_log;
+                if (p != 0.f || z == -INFINITY)
+                    loss += log_q == -INFINITY && z == -INFINITY ? INFINITY : p * ((t - t_log) - log_q);
             }
             list.t[j] = p;
         }
@@ -327,7 +330,7 @@ __device__ __forceinline__ void write_row(const DistillArgs &a, uint32_t r, cons
 #pragma unroll
     for (int w = 0; w < W; w++)
         sum += parts[w];
-    a.loss[r] = some ? a.temperature * a.temperature * sum : 0.f;
+    a.loss[r] = some ? a.temperature * sum : 0.f;
     if (a.row_max) {
         a.row_max[r] = z_max;
         a.row_sum[r] = z_sum;
@@ -789,7 +792,7 @@ static int check_distill(const tmask_distill_desc *desc, tmask_dtype dt, tmask_d
     a.hash_shift = 31;
     while (a.hash_shift > 0 && (1u << (32u - a.hash_shift)) < 2u * a.k)
         a.hash_shift--;
-    a.temperature = temperature; a.per_t = 1.f / temperature; a.per_t2 = (float)(1.4426950408889634 / (double)temperature);
+    a.temperature = temperature; a.per_t2 = (float)(1.4426950408889634 / (double)temperature);
     return TMASK_OK;
 }
 

@@ -464,6 +464,24 @@ def test_distill_masked_logits(vocab, low):
             distill_call(Maker(7), 4, vocab, 8, dt, T=T, edit=edit)
 
 
+@pytest.mark.parametrize("rows,vocab", [(4, 50), (4, 3000), (4, 100000), (300, 4500), (300, 9000), (130, 65700)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [0.25, 0.5, 1.0])
+def test_distill_entries_at_the_lowest_value(T, dt, rows, vocab):
+    """Entries whose logits are the type's lowest, divided by a temperature below 1 beyond all numbers: the teacher's adds nothing,
+    whatever the student's is, and the student's where the teacher has a share costs a large number, not an infinite one."""
+    def edit(z, teacher, index):
+        low = torch.finfo(z.dtype).min
+        index.copy_(torch.arange(index.shape[1], device="cuda").expand_as(index))
+        z[1:3, vocab // 3:] = low
+        index[1:3, 3] = vocab - 1
+        teacher[:2, 3] = low                                    # row 0: the teacher's alone; row 1: both
+        teacher[2, 3] = 0.5                                     # row 2: the student's alone
+        teacher[3, 1:] = low                                    # row 3: one entry has all of it
+    loss = distill_call(Maker(7), rows, vocab, 8, dt, T=T, edit=edit)[3]
+    assert bool(loss.isfinite().all())
+
+
 @pytest.mark.parametrize("vocab", [50, 3000, 100000])
 def test_distill_all_logits_at_the_lowest_value(vocab):
     """A row that holds one value, however low, is the uniform distribution."""
