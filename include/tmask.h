@@ -351,7 +351,8 @@ int tmask_nm_sparse_probability(int N, int M, double rho, double *prob);
  * their gradients, `param_dt` that of weight, bias and their gradients.  All arithmetic is in fp32 and rounded once, to nearest
  * even, where a result is stored; sums are added up in an order that depends on the sizes (and, for the loss, on where rows
  * begin relative to 16 bytes, for column sums on whether an output lies over an input) and on nothing else, so the same call
- * gives the same bits.  An output may be one of the call's inputs of the same type, shape and leading dimension (in place); any
+ * gives the same bits.  The sizes of workspaces grow with both of their arguments: one for a program's longest batch and widest rows serves all of
+ * its calls.  An output may be one of the call's inputs of the same type, shape and leading dimension (in place); any
  * other overlap is not allowed.  NaN and Inf go through the formulas.
  */
 
@@ -446,8 +447,8 @@ size_t tmask_bias_gelu_workspace_bytes(int64_t rows, int64_t cols);          /* 
  * gradient follow from them later; row_max ignores NaN).
  * dlogits is nullable: without it the call gives the loss alone.  row_weight (nullable: 1) is the weight of the row's loss in what is
  * differentiated, such as 1 / tokens.  teacher is of teacher_dt, index of 32 or 64 bits (index_bits).  0 <= k <= 1024; 1e-18 <= T <= 1e18.
- * The workspace (256-byte aligned, tmask_distill_workspace_bytes(rows, vocab), which is 0 for sizes that need none) serves
- * tmask_distill alone.
+ * The workspace (256-byte aligned, tmask_distill_workspace_bytes(rows, vocab), which is 0 where no call of up to so many rows needs one)
+ * serves tmask_distill alone, and only calls of few long rows (fewer than 128) read it.
  */
 typedef struct {
     const void *logits; int64_t ld_logits;

@@ -515,17 +515,17 @@ def _device_bytes(n: int, like: torch.Tensor) -> torch.Tensor:
 
 
 def alloc_layer_norm_workspace(x: torch.Tensor) -> torch.Tensor:
-    """Workspace for tmask_layer_norm_backward of tensors of x's shape."""
+    """Workspace for tmask_layer_norm_backward of tensors of x's shape, or of fewer rows or columns."""
     return _device_bytes(int(load_library().tmask_layer_norm_workspace_bytes(x.shape[0], x.shape[1])), x)
 
 
 def alloc_bias_gelu_workspace(x: torch.Tensor) -> torch.Tensor:
-    """Workspace for tmask_bias_gelu_backward of tensors of x's shape."""
+    """Workspace for tmask_bias_gelu_backward of tensors of x's shape, or of fewer rows or columns."""
     return _device_bytes(int(load_library().tmask_bias_gelu_workspace_bytes(x.shape[0], x.shape[1])), x)
 
 
 def alloc_distill_workspace(logits: torch.Tensor) -> torch.Tensor:
-    """Workspace for tmask_distill of logits of this shape."""
+    """Workspace for tmask_distill of logits of this shape, or of fewer rows or columns."""
     return _device_bytes(int(load_library().tmask_distill_workspace_bytes(logits.shape[0], logits.shape[1])), logits)
 
 

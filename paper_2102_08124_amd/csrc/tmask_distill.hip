@@ -748,15 +748,17 @@ static Cut cut_rows(int64_t rows, uint32_t chunks, uint32_t least, uint32_t most
 
 static uint32_t chunks_of(int64_t vocab, tmask_dtype dt) { return (uint32_t)(vocab / (dt == TMASK_F32 ? 4 : 8)); }   // of a row at most
 
+// Rows of so many chunks are cut in parts if there are fewer than this.  A second launch costs 3 us; a row in one workgroup longer, the longer it is and
+// the fewer compute units have one (us, row / parts: 16 rows of 32000 bf16 8.4 / 10.0, of 64000 11.9 / 10.1; 64 rows of 64000 12.6 / 15.4, of
+// 131072 21.1 / 15.0; 128 of 89000 17.1 / 18.1, of 131072 fp32 32.1 / 35.6; 256 57.7 / 69.4).
+static int64_t cut_below(uint32_t chunks) { return chunks <= 4096 ? 0 : chunks <= kFewHeld ? 64 : 128; }
+
+constexpr uint32_t kLeast = 512, kMost = kAhead * kSlice;                       // chunks of a part
+
 static Cut cut_loss(int64_t rows, int64_t vocab, tmask_dtype dt)
 {
     const uint32_t chunks = chunks_of(vocab, dt);
-    // A second launch costs 3 us; a row in one workgroup longer, the longer it is and the fewer compute units have one (us, row / parts:
-    // 16 rows of 32000 bf16 8.4 / 10.0, of 64000 11.9 / 10.1; 64 rows of 64000 12.6 / 15.4, of 131072 21.1 / 15.0; 128 of 89000 17.1 / 18.1, of
-    // 131072 fp32 32.1 / 35.6; 256 57.7 / 69.4).
-    if (chunks <= 4096 || rows >= (chunks <= kFewHeld ? 64 : 128))
-        return {0, 0};
-    return cut_rows(rows, chunks, 512, kAhead * kSlice);
+    return rows < cut_below(chunks) ? cut_rows(rows, chunks, kLeast, kMost) : Cut{0, 0};
 }
 
 static uint32_t grid_of(uint64_t workgroups) { return (uint32_t)(workgroups < (1u << 20) ? workgroups : 1u << 20); }
@@ -800,18 +802,16 @@ static int check_distill(const tmask_distill_desc *desc, tmask_dtype dt, tmask_d
 
 using namespace tmask;
 
-// Sizes that take parts need, for both types, room for the statistics of every part and a list's logits for every row.
+// Rows that are cut in parts need room for the statistics of every part and for a list's logits.  The size is a bound for all calls of up to so many
+// rows, of either type: as many rows as are cut at all, of fp32's chunks, with the parts that cut_rows may give them.
 extern "C" size_t tmask_distill_workspace_bytes(int64_t rows, int64_t vocab)
 {
-    if (!valid_sizes(rows, vocab) || rows == 0)
+    if (!valid_sizes(rows, vocab))
         return 0;
-    size_t most = 0;
-    for (const tmask_dtype dt : {TMASK_F32, TMASK_BF16}) {
-        const size_t parts = cut_loss(rows, vocab, dt).parts;
-        const size_t need = parts ? (size_t)rows * (2u * parts + kMaxEntries) * 4u : 0;
-        most = need > most ? need : most;
-    }
-    return most;
+    const uint32_t chunks = chunks_of(vocab, TMASK_F32);
+    const uint64_t below = (uint64_t)cut_below(chunks), cut = below == 0 ? 0 : (uint64_t)rows < below ? (uint64_t)rows : below - 1;
+    const uint64_t lower = (chunks + (uint64_t)kMost - 1) / kMost, most = cut * kMaxParts, parts = cut * lower > 1024 ? cut * lower : 1024;
+    return (size_t)(cut * kMaxEntries + 2u * (parts < most ? parts : most)) * 4u;
 }
 
 extern "C" int tmask_distill(const tmask_distill_desc *desc, tmask_dtype dt, tmask_dtype teacher_dt, int index_bits, float temperature,
@@ -868,7 +868,7 @@ extern "C" int tmask_distill_backward(const tmask_distill_desc *desc, tmask_dtyp
     TMASK_TRY(check_vector("row_max", desc->row_max, 4, true));
     TMASK_TRY(check_vector("row_sum", desc->row_sum, 4, true));
     TMASK_TRY(check_rows("dlogits", desc->dlogits, desc->ld_dlogits, desc->rows, desc->vocab, size_of(dt), true));
-    const Cut cut = cut_rows(desc->rows, chunks_of(desc->vocab, dt), 512, kAhead * kSlice);
+    const Cut cut = cut_rows(desc->rows, chunks_of(desc->vocab, dt), kLeast, kMost);
     a.parts = cut.parts;
     a.part_chunks = cut.part_chunks;
     hipLaunchKernelGGL((dt == TMASK_BF16 ? distill_slice_kernel<kBF16, false> : distill_slice_kernel<kF32, false>),

@@ -950,11 +950,13 @@ static bool columns_apart(const tmask_norm_grad_desc &d, size_t size, size_t psi
 
 static uint32_t pitch_of(int64_t cols) { return (uint32_t)((cols + 7) & ~7ll); }      // whole chunks of either type
 
+constexpr uint32_t kLongStrips = 64;                                            // of rows that no workgroup holds
+
 static uint32_t norm_strips(int64_t rows, int64_t cols)
 {
     const NormGradShape *const s = shape_for(kNormGradShapes, cols);
     if (!s)
-        return at_most(rows, 64);
+        return at_most(rows, kLongStrips);
     // Two rounds of one workgroup cost less than a second launch (16 rows of 1024 bf16: 5.1 us, with it 7.2; four rounds 7.5 and 7.3).
     const uint64_t rounds = (rows + s->rows - 1) / s->rows;
     if (rounds <= 2)
@@ -1057,9 +1059,22 @@ extern "C" int tmask_layer_norm(const tmask_norm_desc *desc, tmask_dtype dt, tma
     return launched("layer norm launch");
 }
 
+// Strips' sums of one vector, in floats: at least what norm_strips gives for up to so many rows and columns.
+static size_t norm_sums(int64_t rows, int64_t cols)
+{
+    const NormGradShape *const s = shape_for(kNormGradShapes, cols);
+    if (!s) {
+        const size_t held = norm_sums(rows, kNormGradShapes[sizeof kNormGradShapes / sizeof *kNormGradShapes - 1].cols);
+        const size_t own = (size_t)at_most(rows, kLongStrips) * pitch_of(cols);
+        return held > own ? held : own;
+    }
+    const uint64_t rounds = (rows + s->rows - 1) / s->rows;
+    return (size_t)at_most(rounds, rounds <= 2 ? 1 : kGradStrips) * pitch_of(cols);
+}
+
 extern "C" size_t tmask_layer_norm_workspace_bytes(int64_t rows, int64_t cols)
 {
-    return norm_sizes(rows, cols) ? (size_t)norm_strips(rows, cols) * 2u * pitch_of(cols) * 4u : 0;
+    return norm_sizes(rows, cols) ? 2u * norm_sums(rows, cols) * 4u : 0;
 }
 
 extern "C" int tmask_layer_norm_backward(const tmask_norm_grad_desc *desc, tmask_dtype dt, tmask_dtype param_dt, void *workspace,
@@ -1138,17 +1153,15 @@ extern "C" int tmask_bias_gelu(const tmask_gelu_desc *desc, tmask_dtype dt, tmas
     return launched("GELU launch");
 }
 
+// At least what gelu_tile needs for up to so many rows and columns of either type: one strip, or strips of four rows and more and, with
+// the workgroups beside each other, at most kGradStrips workgroups of at most 256 chunks.
 extern "C" size_t tmask_bias_gelu_workspace_bytes(int64_t rows, int64_t cols)
 {
-    if (!norm_sizes(rows, cols))
+    if (!norm_sizes(rows, cols) || rows == 0)
         return 0;
-    size_t strips = 0;
-    for (const tmask_dtype dt : {TMASK_F32, TMASK_BF16}) {
-        GeluArgs p;
-        gelu_tile(rows, cols, dt, true, &p);
-        strips = p.strips > strips ? p.strips : strips;
-    }
-    return strips * pitch_of(cols) * 4u;
+    constexpr uint64_t kMost = (uint64_t)kGradStrips * 256u * kElems<kBF16>;
+    const uint64_t pitch = pitch_of(cols), strips = ((uint64_t)rows + kGradThreads / 256 - 1) / (kGradThreads / 256), all = strips * pitch;
+    return (size_t)(all < kMost ? all : kMost > pitch ? kMost : pitch) * 4u;
 }
 
 extern "C" int tmask_bias_gelu_backward(const tmask_gelu_grad_desc *desc, tmask_dtype dt, tmask_dtype param_dt, tmask_gelu_form form,

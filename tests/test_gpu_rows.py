@@ -567,6 +567,47 @@ def test_distill_longest_rows_keep_to_themselves(dt):
     assert loss[11] == float("inf") and dz[11, 140000] == 1.0                   # one column left, and not one of the list's
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("most,rows,cols", [(4104, 4096, 1024), (700, 500, 5000), (9000, 64, 100), (300, 200, 16391)])
+def test_gradients_of_a_shorter_batch_in_the_same_workspace(most, rows, cols, dt):
+    """A workspace for the longest batch serves shorter ones, and no call writes behind the size it has for its own."""
+    m = Maker(rows)
+    for alloc, size in ((tm.alloc_layer_norm_workspace, "tmask_layer_norm_workspace_bytes"), (tm.alloc_bias_gelu_workspace, "tmask_bias_gelu_workspace_bytes")):
+        ws = alloc(torch.empty((most, cols), dtype=TYPES[dt], device="cuda"))
+        x, dy = m.normal((rows, cols), TYPES[dt]), m.normal((rows, cols), TYPES[dt])
+        dw, db, dx, mu, rs = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda"), torch.empty_like(x), x.float().mean(1), torch.ones(rows, device="cuda")
+        own = int(getattr(tm.load_library(), size)(rows, cols))
+        ws.fill_(77)
+        if "norm" in size:
+            tm.tmask_layer_norm_backward(dy, x, mu, rs, dx, dweight=dw, dbias=db, workspace=ws)
+            want = refs.layer_norm_backward(np64(dy), np64(x), np64(mu), np64(rs))
+        else:
+            tm.tmask_bias_gelu_backward(dy, x, dx, dbias=db, workspace=ws)
+            want = refs.bias_gelu_backward(np64(dy), np64(x))
+        torch.cuda.synchronize()
+        check(dx, want["dx"], "dx")
+        check(db, want["dbias"], "dbias")
+        assert bool((ws[own:] == 77).all())
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("most,rows,vocab", [(128, 127, 131072), (200, 5, 70001), (64, 63, 20000), (1000, 1, 200003)])
+def test_losses_of_a_shorter_batch_in_the_same_workspace(most, rows, vocab, dt):
+    m = Maker(rows)
+    ws = tm.alloc_distill_workspace(torch.empty((most, vocab), dtype=TYPES[dt], device="cuda"))
+    z = m.normal((rows, vocab), TYPES[dt], 3.0)
+    teacher, index = lists(m, rows, vocab, 1024, torch.float32, 32)
+    loss, dz = torch.empty(rows, device="cuda"), torch.empty_like(z)
+    own = int(tm.load_library().tmask_distill_workspace_bytes(rows, vocab))
+    ws.fill_(77)
+    tm.tmask_distill(z, teacher, index, 1.0, loss, dlogits=dz, workspace=ws)
+    torch.cuda.synchronize()
+    want = refs.distill(np64(z), np64(teacher), index.cpu().numpy(), 1.0)
+    check(loss, want["loss"], "loss")
+    check(dz, want["dlogits"], "dlogits")
+    assert bool((ws[own:] == 77).all())
+
+
 def far(m, rows, cols, dtype):
     """Rows 2^30 + 8 elements apart: the third begins past 2^31 elements (2^32 bytes in bf16, 2^33 in fp32)."""
     pitch = 2 ** 30 + 8

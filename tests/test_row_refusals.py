@@ -109,6 +109,23 @@ def test_workspace_sizes(f):
         assert size(1, 64) >= 256 and size(1 << 20, 1024) <= 64 << 20
 
 
+# around the numbers of rows and columns at which calls are cut otherwise
+BATCHES = [0, 1, 2, 4, 15, 16, 17, 32, 33, 63, 64, 65, 100, 127, 128, 129, 255, 256, 257, 384, 385, 700, 1000, 1024, 1025, 2000, 2048, 2049, 4096, 4104, 5000,
+           8192, 8200, 10000, 12288, 30000, 1 << 20, 1 << 30]
+
+
+@pytest.mark.parametrize("f", ["tmask_layer_norm_workspace_bytes", "tmask_bias_gelu_workspace_bytes", "tmask_distill_workspace_bytes"])
+def test_workspace_sizes_grow_with_both_arguments(f):
+    """So that a program allocates once, for its longest batch and widest rows."""
+    size = getattr(tm.load_library(), f)
+    widths = sorted({max(1, (1 << b) + d) for b in range(21) for d in (-1, 0, 1, 7)} | {1000, 12000, 20000, 40000, 70001, 131072, 200003})
+    table = [[size(r, c) for c in widths] for r in BATCHES]
+    for a, b in zip(table, table[1:]):
+        assert all(x <= y for x, y in zip(a, b))
+    for row in table:
+        assert all(x <= y for x, y in zip(row, row[1:]))
+
+
 def test_tensors_that_do_not_fit():
     """Types and shapes are the binding's to check; host tensors are no tensors of a call."""
     x = torch.zeros((4, 64))
