@@ -737,7 +737,7 @@ __device__ __forceinline__ float gelu(float u)
         q *= t * exponential;
         if constexpr (GRAD)
             return fmaf(u * 0.39894228f, exponential, u < 0.f ? q : 1.f - q);
-        return fmaf(-fminf(a, 100.f), q, fmaxf(u, 0.f));      // u q below 0, u - u q above; q is 0 long before 100, and so +Inf stays
+        return fmaf(-fabsf(fminf(u, 100.f)), q, fmaxf(u, 0.f));   // u q below 0, u - u q above; q is 0 long before 100, and so +Inf stays; -Inf times 0 is NaN
     } else {
         const float u2 = fminf(u * u, 1e4f);                  // the share is 0 or 1 long before; the square stays finite
         const float share = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.3022082f * u * fmaf(0.044715f, u2, 1.f)));

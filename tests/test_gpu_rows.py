@@ -335,6 +335,27 @@ def test_gelu_of_infinities(dt, tanh):
     assert torch.equal(y, y0)
 
 
+@pytest.mark.parametrize("tanh", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_gelu_of_minus_infinity(dt, tanh):
+    """-Inf times a share of 0 is NaN, as is the product in the gradients at both infinities; the neighbours are what they were."""
+    m = Maker(16)
+    x = m.normal((3, 77), TYPES[dt])
+    ones, outs = torch.ones_like(x), []
+    for spoil in (False, True):
+        if spoil:
+            x[1, 5], x[2, 76], x[0, 8] = -float("inf"), -float("inf"), float("inf")
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        tm.tmask_bias_gelu(x, y, tanh=tanh)
+        tm.tmask_bias_gelu_backward(ones, x, dx, tanh=tanh)
+        outs.append((y, dx))
+    torch.cuda.synchronize()
+    (y0, dx0), (y, dx) = outs
+    spoiled = ~x.isfinite()
+    assert bool(y[x == -float("inf")].isnan().all()) and float(y[0, 8]) == float("inf") and bool(dx[spoiled].isnan().all())
+    assert torch.equal(y[~spoiled], y0[~spoiled]) and torch.equal(dx[~spoiled], dx0[~spoiled])
+
+
 @pytest.mark.parametrize("T", [1e-18, 1e-3, 300.0, 1e18])
 def test_distill_temperatures(T):
     """At the ends of their range: the coldest is the largest logit alone, the hottest the uniform distribution.  (Logits are
