@@ -446,11 +446,13 @@ __device__ __forceinline__ void norm_grad_rows(const NormGradArgs p)
     // 221 us; with sums that spill to scratch memory 385), and the weights are read again for each row.
     __shared__ __attribute__((aligned(16))) float kept[2][KEEP || !SUMS ? 4 : kCols];
     const uint32_t lane = threadIdx.x % LANES;
+    // Of a row's chunks the first half is there for every lane: narrower rows have another shape (but for the narrowest).
+    constexpr int kThere = LANES > 8 ? C / 2 : 0;
     uint32_t left[C];
 #pragma unroll
     for (int i = 0; i < C; i++) {
         const uint32_t c = (lane + (uint32_t)(i * LANES)) * N;
-        left[i] = c >= p.cols ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
+        left[i] = i < kThere ? (uint32_t)N : c >= p.cols ? 0u : p.cols - c < (uint32_t)N ? p.cols - c : (uint32_t)N;
     }
     struct Row {
         u32x4 dy[C], x[C], more[C];
@@ -536,7 +538,17 @@ __device__ __forceinline__ void norm_grad_rows(const NormGradArgs p)
                 }
                 d[k] = v[e] * w[at][e];
                 s1 += d[k];
-                s2 += d[k] * h[k];
+            }
+            // Not h of columns that do not exist, where the mean times rstd may be beyond all numbers, and 0 times that is none.
+            if (p.cols % N) {
+#pragma unroll
+                for (int e = 0; e < N; e++)
+                    if ((uint32_t)e < left[i])
+                        s2 += d[i * N + e] * h[i * N + e];
+            } else if (left[i]) {
+#pragma unroll
+                for (int e = 0; e < N; e++)
+                    s2 += d[i * N + e] * h[i * N + e];
             }
             if constexpr (SUMS && !KEEP) {
                 store_sums(&kept[0][(lane + (uint32_t)(i * LANES)) * N], dw[0]);
@@ -684,7 +696,7 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_grad_kernel(const Norm
 #pragma unroll
                 for (int e = 0; e < N; e++) {
                     d[e] *= w[e];
-                    h[e] = (h[e] - mean) * rstd;
+                    h[e] = (uint32_t)e < left ? (h[e] - mean) * rstd : 0.f;
                 }
                 f(c, left, d, h);
             }
@@ -693,7 +705,7 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_grad_kernel(const Norm
         each([&](uint32_t, uint32_t, float (&d)[N], float (&h)[N]) {
 #pragma unroll
             for (int e = 0; e < N; e++) {
-                s1 += d[e];                                                     // d is 0 beyond the row
+                s1 += d[e];                                                     // d and h are 0 beyond the row
                 s2 += d[e] * h[e];
             }
         });

@@ -239,6 +239,23 @@ def test_norm_grad_in_place(cols, in_place):
     grad_call(Maker(6), 70, cols, "bf16", "f32", in_place=in_place)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (5, 1), (3000, 1), (5, 60), (5, 100), (2000, 100), (5, 1001), (1100, 1001), (300, 5000), (5, 12000), (700, 12001), (3, 20001)])
+def test_norm_grad_of_rows_that_hold_one_large_value(rows, cols, dt):
+    """What was normalised is its mean everywhere, so h is 0 and the gradient finite; the columns that a row does not have count for nothing,
+    though their mean times rstd is beyond all numbers."""
+    m = Maker(rows)
+    x = torch.full((rows, cols), 2.0 ** 124, dtype=TYPES[dt], device="cuda")
+    dy, w = m.normal((rows, cols), TYPES[dt], 0.3), m.normal((cols,), torch.float32, 0.2, 1.0)
+    mu, rs = torch.full((rows,), 2.0 ** 124, device="cuda"), torch.full((rows,), 316.0, device="cuda")
+    dx, dw, db = torch.empty_like(x), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    tm.tmask_layer_norm_backward(dy, x, mu, rs, dx, w, dweight=dw, dbias=db, workspace=tm.alloc_layer_norm_workspace(x))
+    torch.cuda.synchronize()
+    want = refs.layer_norm_backward(np64(dy), np64(x), np64(mu), np64(rs), np64(w))
+    for name, got in (("dx", dx), ("dweight", dw), ("dbias", db)):
+        check(got, want[name], name)
+
+
 @pytest.mark.parametrize("which", ["dweight", "dbias"])
 def test_norm_grad_of_one_parameter(which):
     m = Maker(8)
