@@ -753,8 +753,13 @@ __device__ __forceinline__ float gelu(float u)
         return fmaf(-fabsf(fminf(u, 100.f)), q, fmaxf(u, 0.f));   // u q below 0, u - u q above; q is 0 long before 100, and so +Inf stays; -Inf times 0 is NaN
     } else {
         const float u2 = fminf(u * u, 1e4f);                  // the share is 0 or 1 long before; the square stays finite
-        const float share = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.3022082f * u * fmaf(0.044715f, u2, 1.f)));
-        return GRAD ? fmaf(u * (share * (1.f - share)) * 1.5957691f, fmaf(0.134145f, u2, 1.f), share) : u * share;
+        if constexpr (GRAD) {
+            // From |u|: the smaller of share and 1 - share is e t, to its own size (with share - share^2 the derivative was off by 2e-6 near u = 3.5).
+            const float e = __builtin_amdgcn_exp2f(-2.3022082f * fabsf(u) * fmaf(0.044715f, u2, 1.f));
+            const float t = __builtin_amdgcn_rcpf(1.f + e), less = e * t;
+            return fmaf(u * (less * t) * 1.5957691f, fmaf(0.134145f, u2, 1.f), u < 0.f ? less : t);
+        }
+        return u * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.3022082f * u * fmaf(0.044715f, u2, 1.f)));
     }
 }
 

@@ -335,6 +335,24 @@ def test_gelu_everywhere(tanh):
         check(dx, (slope, 16 * refs.U * (1 + np.minimum(np.abs(u), 20.0))), "dx")
 
 
+def test_gelu_tanh_slope_where_the_share_is_near_one():
+    """The derivative's second term has share (1 - share) as a factor, which has to be as good as its own size.  With e = exp(-a), a = 2 |s|, and
+    t = 1 / (1 + e), each rounded operation u: e is off by (6 a + 2) u, t by 3 u and e t times that, u e t^2 and its factors by
+    (12 a + 18) u, the share (t or e t) by 4 u and three times 1 - share of e's; what is below the least normal number may be lost."""
+    x = torch.linspace(-12.0, 12.0, 1 << 20, device="cuda").reshape(1024, 1024)
+    dx = torch.empty_like(x)
+    tm.tmask_bias_gelu_backward(torch.ones_like(x), x, dx, tanh=True)
+    torch.cuda.synchronize()
+    u = np64(x)
+    s = np.sqrt(2 / np.pi) * (u + 0.044715 * u ** 3)
+    a, share, rest = 2 * np.abs(s), 1 / (1 + np.exp(-2 * s)), 1 / (1 + np.exp(2 * s))
+    factor = 2 * u * np.sqrt(2 / np.pi) * (1 + 3 * 0.044715 * u ** 2)
+    second = factor * share * rest
+    slope = share + second
+    off = np.abs(second) * (12 * a + 18) + share * (4 + 3 * rest * (6 * a + 2)) + np.abs(slope)
+    check(dx, (slope, refs.U * off + 2.0 ** -126 * (1 + np.abs(factor))), "dx")
+
+
 @pytest.mark.parametrize("tanh", [False, True])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_gelu_of_infinities(dt, tanh):
