@@ -867,7 +867,7 @@ __global__ void __launch_bounds__(kGeluThreads<GRAD>) gelu_kernel(const GeluArgs
 }
 
 // Adds up the strips' sums: 8 lanes take 32 neighbouring columns (a line of 128 bytes), 32 of these groups every 32nd strip.  Latency:
-// 3 to 4 us, whatever the size up to 256 strips of 4096 columns.
+// 3 to 4 us, whatever the size up to 256 strips of 4096 columns.  There are kGradStrips at most: norm_strips and gelu_tile give no more.
 __global__ void __launch_bounds__(kThreads) columns_kernel(const ColumnArgs p)
 {
     void *const out = p.out[blockIdx.y];
@@ -879,7 +879,7 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(const ColumnArgs p)
     if (c < p.cols && p.strips) {                                               // the pitch is a multiple of eight
         const float *const from = p.partial + (size_t)blockIdx.y * p.pitch + c;
         const size_t row = (size_t)p.sums * p.pitch;
-        constexpr int kAll = kGradStrips / 32;                                  // all in flight together
+        constexpr int kAll = kGradStrips / 32;                                  // all there can be, in flight together
         f32x4 v[kAll];
 #pragma unroll
         for (int i = 0; i < kAll; i++) {
@@ -890,8 +890,6 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(const ColumnArgs p)
         for (int i = 0; i < kAll; i++)
             if (y + (uint32_t)i * 32u < p.strips)
                 s += v[i];
-        for (uint32_t k = kGradStrips + y; k < p.strips; k += 32u)
-            s += *(const f32x4 *)(from + k * row);
     }
 #pragma unroll
     for (int e = 0; e < 4; e++)
@@ -969,6 +967,7 @@ static bool columns_apart(const tmask_norm_grad_desc &d, size_t size, size_t psi
 static uint32_t pitch_of(int64_t cols) { return (uint32_t)((cols + 7) & ~7ll); }      // whole chunks of either type
 
 constexpr uint32_t kLongStrips = 64;                                            // of rows that no workgroup holds
+static_assert(kLongStrips <= kGradStrips && kGradStrips % 32 == 0, "what columns_kernel adds up");
 
 static uint32_t norm_strips(int64_t rows, int64_t cols)
 {
