@@ -54,7 +54,8 @@ __device__ __forceinline__ List list_in(void *lds, const DistillArgs &a)
     return l;
 }
 
-static size_t list_bytes(uint32_t k, uint32_t hash_shift) { return 4u * (4u + 3u * k + (k ? 1u << (32u - hash_shift) : 0u)); }
+// of LDS; `table`: with room for it
+static size_t list_bytes(const DistillArgs &a, bool table) { return 4u * (4u + 3u * a.k + (a.k && table ? 1u << (32u - a.hash_shift) : 0u)); }
 
 // exp(x / T) for x <= 0
 __device__ __forceinline__ float exp_of(const DistillArgs &a, float x) { return __builtin_amdgcn_exp2f(x * a.per_t2); }
@@ -382,7 +383,7 @@ __device__ __forceinline__ void distill_row(const DistillArgs a)
                                              threadIdx.x * 16u);
             }
         };
-        if (a.k) {
+        if (a.k && a.dlogits) {
             clear_table<T>(a, list);
             __syncthreads();
         }
@@ -826,7 +827,7 @@ extern "C" int tmask_distill(const tmask_distill_desc *desc, tmask_dtype dt, tma
     TMASK_TRY(check_vector("row_sum", desc->row_sum, 4, desc->row_max != nullptr));
     hipStream_t stream = (hipStream_t)hip_stream;
     const Cut cut = cut_loss(desc->rows, desc->vocab, dt);
-    const size_t list = list_bytes(a.k, a.hash_shift);
+    const size_t list = list_bytes(a, a.dlogits != nullptr);                     // the loss alone does not mind repeats
     const bool bf16 = dt == TMASK_BF16;
     if (cut.parts == 0 && !a.dlogits && desc->rows > kFew && chunks_of(desc->vocab, dt) > kLossHeld) {
         a.parts = 1;
@@ -872,6 +873,6 @@ extern "C" int tmask_distill_backward(const tmask_distill_desc *desc, tmask_dtyp
     a.parts = cut.parts;
     a.part_chunks = cut.part_chunks;
     hipLaunchKernelGGL((dt == TMASK_BF16 ? distill_slice_kernel<kBF16, false> : distill_slice_kernel<kF32, false>),
-                       dim3(grid_of((uint64_t)a.rows * a.parts)), dim3(kSlice), 20 * (kSlice / 64) + list_bytes(a.k, a.hash_shift), (hipStream_t)hip_stream, a);
+                       dim3(grid_of((uint64_t)a.rows * a.parts)), dim3(kSlice), 20 * (kSlice / 64) + list_bytes(a, true), (hipStream_t)hip_stream, a);
     return launched("distillation gradient launch");
 }
