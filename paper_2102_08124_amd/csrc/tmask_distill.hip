@@ -184,7 +184,9 @@ __device__ __forceinline__ void clear_table(const DistillArgs &a, const List &l)
         *l.repeats = 0;
 }
 
-// what the entries take from column `at`: the sum of their probabilities, in the list's order
+// What the entries take from column `at`: the sum of their probabilities, in the list's order.  In a row with a repeat every entry adds up so, k LDS
+// reads each, in a fixed order and without atomics: a teacher's largest logits hold none, and a list that does costs k^2 (4096 rows of 32000 bf16 with one
+// repeat each 105 us at k = 64, 167 at 256, 1110 at 1000, without 102, 146 and 232; 8000 rows of 500 24 and 152 at k = 64 and 250, without 15 and 19).
 __device__ __forceinline__ float share_of(const DistillArgs &a, const List &l, int32_t at)
 {
     float s = 0.f;

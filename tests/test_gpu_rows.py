@@ -406,6 +406,28 @@ def test_distill_temperatures(T):
     assert bool(loss.isfinite().all()) or T == 1e18
 
 
+@pytest.mark.parametrize("T", [1e-18, 1e-3, 0.3, 300.0, 1e18])
+def test_distill_losses_at_temperatures(T):
+    """The list has two of 60 columns, so the hottest loss tends to T^2 log 30 and is a number at either end."""
+    z = torch.arange(60, device="cuda", dtype=torch.float32).flip(0).reshape(1, -1)
+    teacher, index = torch.tensor([[2.0, 1.0]], device="cuda"), torch.tensor([[3, 0]], device="cuda", dtype=torch.int32)
+    loss, later = torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    tm.tmask_distill(z, teacher, index, T, loss)
+    tm.tmask_distill(z, teacher, index, T, later, dlogits=torch.empty_like(z))
+    torch.cuda.synchronize()
+    want = refs.distill(np64(z), np64(teacher), index.cpu().numpy(), T)
+    check(loss, want["loss"], "loss")
+    check(later, want["loss"], "loss")
+
+
+@pytest.mark.parametrize("T", [1.0, 30.0, 1000.0])
+def test_distill_losses_of_lists_that_hold_the_vocabulary(T):
+    """The hotter, the more the two logarithms cancel: the loss is as good as T^2 times what they are rounded by, and no better."""
+    def edit(z, teacher, index):
+        index.copy_(torch.arange(index.shape[1], device="cuda").expand_as(index))
+    distill_call(Maker(5), 3, 1000, 1000, "f32", T=T, edit=edit)
+
+
 def test_gelu_in_place():
     m = Maker(4)
     x, dy = m.normal((9, 777), torch.bfloat16), m.normal((9, 777), torch.bfloat16)
