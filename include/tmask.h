@@ -441,10 +441,10 @@ size_t tmask_bias_gelu_workspace_bytes(int64_t rows, int64_t cols);          /* 
  *     loss[r] = T^2 sum_j p_j (log p_j - log q_index(j))
  *     dlogits[r][v] = row_weight[r] * T * (q_v - sum of p_j over the entries with index(j) = v)
  * A row without an entry has loss 0 and gradient 0; a row whose weight is 0 (padding) has gradient 0 whatever its logits are.
- * An index that is given several times counts several times (and costs the gradient's row time of order k^2).  A masked logit (-Inf or the type's lowest value) has q = 0: an entry
- * for which the student has q = 0 by -Inf makes the loss +Inf, the gradient stays finite; by the lowest value the loss is as large as the
- * formula has it.  An entry whose p is below the least normal number of fp32 adds nothing otherwise.  Logits that hold NaN or +Inf, or nothing but -Inf, make
- * the row's loss and gradient NaN.
+ * An index that is given several times counts several times (and costs the gradient's row time of order k^2).  A masked logit (-Inf or
+ * the type's lowest value) has q = 0: an entry for which the student has q = 0 by -Inf makes the loss +Inf, the gradient stays finite; by the
+ * lowest value the loss is as large as the formula has it.  An entry whose p is below the least normal number of fp32 adds nothing otherwise.
+ * Logits that hold NaN or +Inf, or nothing but -Inf, make the row's loss and gradient NaN.
  * The loss is T^2 times a difference of logarithms, each good to about 2^-23 of its size: where p and q nearly agree (a list of nearly all
  * the vocabulary, at a high temperature) its error is that of a number of size T^2 log(vocab), 1e-2 at T = 100.
  * row_max[r] = max_v z, row_sum[r] = sum_v exp((z_v - row_max) / T): nullable outputs, both or neither (q and the

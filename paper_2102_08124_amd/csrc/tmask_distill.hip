@@ -477,7 +477,8 @@ __global__ void __launch_bounds__(kLong) distill_long_kernel(const DistillArgs a
 // Few long rows: parts of rows.  The first launch takes the maximum and the sum of each part and the
 // student's logits of the entries in it; the second joins them and does the rest, part by part, from logits that the caches may
 // still hold.  48 rows of 131072 fp32, loss and gradient: 7 and 10 us (25 MB read, then 25 read from the caches and 25 written).
-// A gradient alone has its statistics and needs the second launch only: 1003 rows of 50021 bf16 43 us (4.6 TB/s).
+// A gradient alone has its statistics and needs the second launch only: 1003 rows of 50021 bf16 43 us (4.6 TB/s).  Its 256 threads are
+// too many for short rows, a part each: 8000 rows of 500 bf16 41 us, 4000 of 2304 fp32 28, where loss and gradient in one call take 14 and 17.
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kAhead = 8;                 // chunks that a thread has in flight
 
@@ -710,6 +711,8 @@ struct RowKernel {
 };
 
 #define ROW_KERNEL(T, P, ABOVE) {T, T * P, ABOVE, {distill_row_kernel<kF32, T, P>, distill_row_kernel<kBF16, T, P>}}
+// Short rows are bound by a row's chain of latencies (entries, their logits, two sums, the columns that the list names): 8000 rows of 500 bf16 take 14 us, of which
+// 2.9 are what so many empty workgroups take, with the vector ALU busy for 36 %.
 // A compute unit holds several of the smaller workgroups, which overlap one row's loads with another's arithmetic: with many rows they win
 // (2048 rows of 15000 bf16: 256 threads with 8 chunks each 31 us, 1024 with 4 58).  Up to a row for each of 256 compute units nothing
 // overlaps, and a row is done soonest by many threads (64 rows of 8000 bf16: 64 threads with 16 chunks 10.1 us, 1024 with 4 6.8).  In between

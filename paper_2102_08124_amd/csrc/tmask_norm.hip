@@ -268,7 +268,8 @@ __global__ void __launch_bounds__(kNormThreads<LANES>) norm_kernel(const NormArg
     }
 }
 
-// Rows that no workgroup holds: three passes, the second and third through the caches.
+// Rows that no workgroup holds: three passes, the second and third through the caches, with one chunk of a thread in flight.  Bound by those loads'
+// latency: 4000 rows of 20480 bf16 with a residual and its sum 192 us, of which 131 are what has to be moved.
 constexpr int kLongThreads = 1024;
 
 template <int DT>
@@ -442,8 +443,8 @@ __device__ __forceinline__ void norm_grad_rows(const NormGradArgs p)
     constexpr int kShared = LANES < 64 ? W : kRows;                             // sets of column sums that the workgroup adds up
     constexpr bool MORE = DT == kBF16 || LANES < 1024;                          // dtotal ahead too: 128 registers do not hold it besides
     __shared__ float red[2][2 * W];
-    // Rows twice as wide as the registers take with all that: the sums lie in LDS, each thread's in its own places (4000 rows of 16000 fp32
-    // 221 us; with sums that spill to scratch memory 385), and the weights are read again for each row.
+    // Rows twice as wide as the registers take with all that: the sums lie in LDS, each thread's in its own places (4000 rows of 16000 fp32 with
+    // dtotal 209 us, 4.9 TB/s; with sums that spill to scratch memory 385), and the weights are read again for each row.
     __shared__ __attribute__((aligned(16))) float kept[2][KEEP || !SUMS ? 4 : kCols];
     const uint32_t lane = threadIdx.x % LANES;
     // Of a row's chunks the first half is there for every lane: narrower rows have another shape (but for the narrowest).
@@ -656,7 +657,8 @@ __global__ void __launch_bounds__(kGradThreads) norm_short_grad_kernel(const Nor
         norm_grad_columns<DT, (int)apart_lanes<DT>(LANES * E)>(p, blockIdx.x - p.strips);
 }
 
-// Rows that no workgroup holds: the sums over rows first (dx may lie over dy or x), a column a thread, then dx in two passes.
+// Rows that no workgroup holds: the sums over rows first (dx may lie over dy or x), a column a thread, then dx in two passes.  4000 rows of 20480 bf16
+// with dtotal 266 us (112 for the sums, by loads of one element, and 149), of which 131 are what has to be moved.
 template <int DT>
 __global__ void __launch_bounds__(kThreads) norm_long_columns_kernel(const NormGradArgs p)
 {
@@ -952,8 +954,10 @@ static bool overlaps(const void *a, int64_t ld_a, const void *b, int64_t ld_b, i
     return pa < pb + (size_t)((rows - 1) * ld_b + cols) * size && pb < pa + (size_t)((rows - 1) * ld_a + cols) * size;
 }
 
-// Column sums by workgroups of their own: 200 rows of 1024 bf16 4.7 us (two launches 7.2), of 12000 9.3 (16.3), 1003 of 2051 fp32 11.6 (12.7), of
-// 12000 bf16 31 (36), but 1500 of 1024 10.3 (7.7).  Not where a workgroup would write what another reads.
+// Column sums by workgroups of their own (in parentheses: in a second launch), us: 1024 columns of bf16, 200 rows 3.9 (6.4), 600 4.9 (6.7), 1000 6.2 (6.9), 1200
+// 7.6 (7.1), 1500 9.5 (7.3), of fp32 600 4.6 (6.8), 1000 7.7 (7.3); 4096 columns of bf16, 1000 rows 9.6 (12.0), 1500 13.1 (13.4); 2051 of fp32, 1003 rows 10.5 (11.1),
+// 1500 14.9 (12.8); 12000 of bf16, 200 rows 7.6 (15.2), 1000 22 (30), 1500 31 (40).  One limit for all widths gives away a little on both sides of it.  Not where
+// a workgroup would write what another reads.
 static bool columns_apart(const tmask_norm_grad_desc &d, size_t size, size_t psize)
 {
     if (d.rows > kApartRows)
@@ -980,13 +984,16 @@ static uint32_t norm_strips(int64_t rows, int64_t cols)
         return at_most(rounds, 1);
     if (rounds <= kGradStrips)
         return (uint32_t)rounds;
-    // as many rounds for each, where that saves a quarter of the strips (and their sums)
+    // As many rounds for each, where that saves a quarter of the strips (and their sums): 2200 rows of 1024 bf16 on 138 strips 8.4 us, on 256 8.6; 3500 on 219 9.4,
+    // on 256 9.3.
     const uint64_t each = (rounds + kGradStrips - 1) / kGradStrips, even = (rounds + each - 1) / each;
     return even <= kGradStrips * 3 / 4 ? (uint32_t)even : kGradStrips;
 }
 
-// The tile of GELU's kernels: lanes that waste little at the end of a row, but rather many, since short pieces of rows cut more lines
-// (30000 rows of 1400: bf16 in pieces of 16 lanes 49 us, of 64 lanes 40; fp32 of 32 lanes 82, of 128 lanes 72).
+// The tile of GELU's kernels: lanes that waste little at the end of a row, but rather many, since short pieces of rows cut more lines.  `price` is what a place
+// costs with 8 ... 256 lanes, set between rows that begin anywhere, where 8 lanes cost 1.8 and 2.2 times as much as 256, and whole lines, where it is 1.1 (gradients
+// 1.2).  By 8, 16, 32, 64, 128 and 256 lanes, us: 30000 rows of 1400 fp32 103, 89, 80, 75, 71 (taken), 85, bf16 57, 47, 44, 39 (taken), 46, 38; of 1024 fp32 56, 51, 48, 48, 50,
+// 52 (taken), gradients 93, 80, 76, 75, 75, 75 (taken); 8000 rows of 320 fp32 5.3, 5.2 (taken), 5.3, 6.0, 5.9, 5.8, bf16 4.2 (taken), 4.4, 5.7, 5.4, 5.0, 5.2.
 static void gelu_tile(int64_t rows, int64_t cols, tmask_dtype dt, bool grad, GeluArgs *p)
 {
     const uint32_t n = dt == TMASK_F32 ? 4 : 8;
