@@ -443,7 +443,7 @@ size_t tmask_bias_gelu_workspace_bytes(int64_t rows, int64_t cols);          /* 
  * A row without an entry has loss 0 and gradient 0; a row whose weight is 0 (padding) has gradient 0 whatever its logits are.
  * An index that is given several times counts several times (and costs the gradient's row time of order k^2).  A masked logit (-Inf or
  * the type's lowest value) has q = 0: an entry for which the student has q = 0 by -Inf makes the loss +Inf, the gradient stays finite; by the
- * lowest value the loss is as large as the formula has it.  An entry whose p is below the least normal number of fp32 adds nothing otherwise.
+ * lowest value the loss is as large as the formula has it (+Inf beyond fp32).  An entry whose p is below the least normal number of fp32 adds nothing otherwise.
  * Logits that hold NaN or +Inf, or nothing but -Inf, make the row's loss and gradient NaN.
  * The loss is T^2 times a difference of logarithms, each good to about 2^-23 of its size: where p and q nearly agree (a list of nearly all
  * the vocabulary, at a high temperature) its error is that of a number of size T^2 log(vocab), 1e-2 at T = 100.

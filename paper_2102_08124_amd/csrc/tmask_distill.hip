@@ -294,21 +294,21 @@ __device__ __forceinline__ u32x4 pull(const DistillArgs &a, u32x4 raw, float z_m
     return pack<DT>(v);
 }
 
-// Turns the logits of a thread's entries into probabilities; the result is what they add to the loss, in units of T.  With logarithms times T
-// a logit of the type's lowest value stays a number where 1 / T of it is none.  An entry that has lost its probability adds nothing, unless
-// the student's logit is -Inf; so does p log p at p = 0.
+// Turns the logits of a thread's entries into probabilities; the result is what they add to the loss, in units of 4 T.  Everything is a quarter of its size, and
+// logarithms are taken times T: so no difference of finite logits and no sum of their shares of it overflows, where the type's lowest value minus the
+// maximum, times 1 / T, or shared out by shares that add up to 1 and a rounding more, would be infinite, and 0 times that NaN.
 template <uint32_t T, bool LOSS = true>
 __device__ __forceinline__ float take_entries(const DistillArgs &a, const List &list, float t_max, float t_sum, float z_max, float z_sum)
 {
-    const float t_log = LOSS ? a.temperature * logf(t_sum) : 0.f, z_log = LOSS ? a.temperature * logf(z_sum) : 0.f, part = 1.f / t_sum;
+    const float part = 1.f / t_sum, scale = 0.25f * a.temperature;
+    const float t_log = LOSS ? scale * logf(t_sum) : 0.f, z_log = LOSS ? scale * logf(z_sum) : 0.f, t_top = 0.25f * t_max, z_top = 0.25f * z_max;
     float loss = 0.f;
     for (uint32_t j = threadIdx.x; j < a.k; j += T)
         if (list.at[j] >= 0) {
-            const float t = list.t[j] - t_max, p = exp_of(a, t) * part;
+            const float t = list.t[j], p = exp_of(a, t - t_max) * part;
             if constexpr (LOSS) {
-                const float z = list.z[j], log_q = (z - z_max) - z_log;
-                if (p != 0.f || z == -INFINITY)
-                    loss += log_q == -INFINITY && z == -INFINITY ? INFINITY : p * ((t - t_log) - log_q);
+                const float log_q = fmaf(list.z[j], 0.25f, -z_top) - z_log;
+                loss += log_q == -INFINITY ? INFINITY : p * ((fmaf(t, 0.25f, -t_top) - t_log) - log_q);
             }
             list.t[j] = p;
         }
@@ -333,7 +333,7 @@ __device__ __forceinline__ void write_row(const DistillArgs &a, uint32_t r, cons
 #pragma unroll
     for (int w = 0; w < W; w++)
         sum += parts[w];
-    a.loss[r] = some ? a.temperature * sum : 0.f;
+    a.loss[r] = some ? a.temperature * 4.f * sum : 0.f;
     if (a.row_max) {
         a.row_max[r] = z_max;
         a.row_sum[r] = z_sum;

@@ -560,6 +560,30 @@ def test_distill_entries_at_the_lowest_value(T, dt, rows, vocab):
     assert bool(loss.isfinite().all())
 
 
+@pytest.mark.parametrize("rows,vocab", [(300, 50), (300, 4500), (4, 100000)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_distill_lists_on_columns_at_the_lowest_value(dt, rows, vocab):
+    """All of the teacher's mass where the student has the lowest value: shares that add up to 1 and a rounding more do not make it infinite."""
+    def edit(z, teacher, index):
+        index.copy_(torch.arange(index.shape[1], device="cuda").expand_as(index))
+        z[:, :index.shape[1]] = torch.finfo(z.dtype).min
+    loss = distill_call(Maker(8), rows, vocab, 12, dt, T=0.5, edit=edit)[3]
+    assert bool(loss.isfinite().all())
+
+
+@pytest.mark.parametrize("rows,vocab", [(4, 50), (300, 4500), (4, 100000)])
+def test_distill_logits_from_the_lowest_to_the_largest_value(rows, vocab):
+    """Differences of finite logits beyond fp32: of the teacher's, where the lower has no share, and of the student's."""
+    def edit(z, teacher, index):
+        low, high = torch.finfo(torch.float32).min, torch.finfo(torch.float32).max
+        index.copy_(torch.arange(index.shape[1], device="cuda").expand_as(index))
+        teacher[0, 0], teacher[0, 1:] = high, low
+        z[1, 0], z[1, 1:3] = 1e38, low
+        z[3, 7], z[3, 8] = low, high
+    loss, dz = distill_call(Maker(8), rows, vocab, 12, "f32", T=0.25, edit=edit)[3:]
+    assert bool(loss.isfinite().all()) and bool(dz.isfinite().all())
+
+
 @pytest.mark.parametrize("vocab", [50, 3000, 100000])
 def test_distill_all_logits_at_the_lowest_value(vocab):
     """A row that holds one value, however low, is the uniform distribution."""
