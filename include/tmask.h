@@ -405,8 +405,8 @@ size_t tmask_layer_norm_workspace_bytes(int64_t rows, int64_t cols);         /* 
  *     TMASK_GELU_ERF   y = u / 2 * (1 + erf(u / sqrt 2))
  *     TMASK_GELU_TANH  y = u / 2 * (1 + tanh(sqrt(2 / pi) * (u + 0.044715 u^3)))
  * and its gradients: dx = dy * dy/du, dbias (nullable, cols elements of param_dt) = sum_rows dx, from the same x and bias.
- * The share of u that passes is good to 3e-7 of 1: with erf it is not held to its own size where it vanishes (off by 4e-4 of its value at
- * u = -4, by 1e-3 at -5, by 2e-3 at -6).
+ * For fp32 the erf form is as good as one with erf in fp32, and better in the negative tail; for bf16 its share of u that passes is good to 3e-7 of
+ * 1, far below the rounding of the result, but not to its own size where it vanishes (off by 4e-4 of its value at u = -4, 1e-3 at -5, 2e-3 at -6).
  * Finite u give finite results, however large; u = +Inf gives y = +Inf; u = -Inf gives NaN (-Inf times 0), as do both infinities in
  * dy/du.  The workspace (256-byte aligned, tmask_bias_gelu_workspace_bytes(rows, cols)) is needed if dbias is asked for.
  */

@@ -732,17 +732,19 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_grad_kernel(const Norm
 // ---------------------------------------------------------------------------------------------------------------------
 // GELU.  With E(a) = exp(-a^2 / 2), the share Phi(u) = (1 + erf(u / sqrt 2)) / 2 that passes is E(u) R(t) for u < 0 and one minus that of -u for
 // u > 0, t = 1 / (1 + 0.33 |u|): R is a polynomial of degree 5 without constant term, fitted by linear programming for the least difference of E R
-// from the share; it is off by at most 9.2e-8 (the least of all such is 6.6e-8, which the roundings of v_rcp, v_exp and the products hide: for
-// 0 < u < 1 y is off by 4.3e-7 of its value, with an erf in fp32 by 1.5e-7, the derivative by 2.5e-7 and 1.5e-7).  The derivative
-// Phi(u) + u E(u) / sqrt(2 pi) has the same exponential.  The form with tanh is the share 1 / (1 + exp(-2 s)).
+// from the share; it is off by at most 9.2e-8 (the least of all such is 6.6e-8, which the roundings of v_rcp, v_exp and the products hide).  That is for
+// bf16, whose rounding is 2e4 times as much.  For fp32 such an R serves from |u| = 1.25 on, where the share's roundings are small, held to
+// 1.3e-5 of its own size in the tail and to 1.4e-8 of 1; below, the share is 1/2 + u times a polynomial of degree 5 in u^2, off by 3.6e-9 (y of 0 < u < 1 is off by 1.2e-7 of its
+// value, with R alone by 4.2e-7, with an erf by 1.4e-7; the derivative by 1.4e-7, 2.5e-7 and 1.5e-7).  The derivative Phi(u) + u E(u) / sqrt(2 pi) has the same
+// exponential.  The form with tanh is the share 1 / (1 + exp(-2 s)).
 //
 // Bound by memory at size, with the vector ALU not far behind: 8192 x 4096 bf16 28.8 us (134 MB, 4.7 TB/s; 16 instructions an element, of which two
 // transcendentals that take four times as long), gradients 43.7 us (201 MB, 4.6 TB/s; 21 instructions).  A library erf instead took 57 us.
 // ---------------------------------------------------------------------------------------------------------------------
-template <int FORM, bool GRAD>
+template <int DT, int FORM, bool GRAD>
 __device__ __forceinline__ float gelu(float u)
 {
-    if constexpr (FORM == TMASK_GELU_ERF) {
+    if constexpr (FORM == TMASK_GELU_ERF && DT == kBF16) {
         const float a = fabsf(u), t = __builtin_amdgcn_rcpf(fmaf(0.33f, a, 1.f));
         const float exponential = __builtin_amdgcn_exp2f(u * u * -0.72134752f);
         float q = fmaf(-0.11074109f, t, 0.37948442f);
@@ -753,6 +755,21 @@ __device__ __forceinline__ float gelu(float u)
         if constexpr (GRAD)
             return fmaf(u * 0.39894228f, exponential, u < 0.f ? q : 1.f - q);
         return fmaf(-fabsf(fminf(u, 100.f)), q, fmaxf(u, 0.f));   // u q below 0, u - u q above; q is 0 long before 100, and so +Inf stays; -Inf times 0 is NaN
+    } else if constexpr (FORM == TMASK_GELU_ERF) {
+        const float a = fabsf(u), u2 = u * u, s = __builtin_amdgcn_rcpf(fmaf(0.4f, a, 1.f));
+        const float exponential = __builtin_amdgcn_exp2f(u2 * -0.72134752f);
+        float far = fmaf(-0.09980094f, s, 0.17087775f);
+        far = fmaf(far, s, 0.10440618f);
+        far = fmaf(far, s, 0.16429004f);
+        far = fmaf(far, s, 0.15929432f);
+        far *= s * exponential;
+        float near = fmaf(-6.6448616e-06f, u2, 0.00011032746f);
+        near = fmaf(near, u2, -0.0011827096f);
+        near = fmaf(near, u2, 0.0099715004f);
+        near = fmaf(near, u2, -0.06648999f);
+        near = fmaf(near, u2, 0.39894226f);
+        const float share = a < 1.25f ? fmaf(u, near, 0.5f) : u < 0.f ? far : 1.f - far;
+        return GRAD ? fmaf(u * 0.39894228f, exponential, share) : u * share;
     } else {
         const float u2 = fminf(u * u, 1e4f);                  // the share is 0 or 1 long before; the square stays finite
         if constexpr (GRAD) {
@@ -822,7 +839,7 @@ __global__ void __launch_bounds__(kGeluThreads<GRAD>) gelu_kernel(const GeluArgs
                     unpack<DT>(settle<DT>(d[i], left, p.cols), u);
 #pragma unroll
                     for (int e = 0; e < N; e++) {
-                        v[e] = gelu<FORM, GRAD>(v[e] + b[e]);
+                        v[e] = gelu<DT, FORM, GRAD>(v[e] + b[e]);
                         if constexpr (GRAD) {
                             v[e] *= u[e];
                             sum[e] += v[e];                                     // 0 beyond the row, where dy is 0 and x and bias are

@@ -43,3 +43,28 @@ def test_the_tail_is_not_as_good_as_its_own_size(source):
     for a, part in ((4.0, 4e-4), (5.0, 1e-3), (6.0, 2e-3)):
         exact = 0.5 * math.erfc(a / math.sqrt(2))
         assert part / 4 < abs(share(source, np.array([a]))[0] - exact) / exact < part
+
+
+def test_the_share_of_fp32_numbers(source):
+    """Both of its polynomials, in 64 bits, with the figures that stand beside them; below 1.25 and from there on."""
+    body = source[source.index("float gelu(float u)"):]
+    scale = float(np.float32(re.search(r"s = __builtin_amdgcn_rcpf\(fmaf\(([\d.]+)f, a, 1\.f\)\)", body).group(1)))
+    number = r"(-?[\d.e-]+)f"
+    coefficients = {name: list(re.search(r"float %s = fmaf\(%s, %s, %s\);" % (name, number, by, number), body).groups()) +
+                    re.findall(r"%s = fmaf\(%s, %s, %s\);" % (name, name, by, number), body) for name, by in (("far", "s"), ("near", "u2"))}
+    assert len(coefficients["far"]) == 5 and len(coefficients["near"]) == 6
+
+    def polynomial(name, x):
+        v = np.zeros_like(x)
+        for k in coefficients[name]:
+            v = v * x + float(np.float32(k))
+        return v
+
+    a = np.linspace(0, 13, 200001)
+    exact = 0.5 * np.vectorize(math.erfc)(a / math.sqrt(2))
+    limit = float(re.search(r"a < ([\d.]+)f \?", body).group(1))
+    near, far = a <= limit, a >= limit
+    t = 1 / (1 + scale * a)
+    off_far = np.abs(polynomial("far", t) * t * np.exp(-0.5 * a * a) - exact)
+    assert np.abs(0.5 - a * polynomial("near", a * a) - exact)[near].max() <= 3.6e-9
+    assert off_far[far].max() <= 1.4e-8 and (off_far / exact)[far].max() <= 1.3e-5
